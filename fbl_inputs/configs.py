@@ -189,3 +189,30 @@ XATTN_CONFIGS = {
     # a small ragged case the oracle finishes in well under a second
     "tiny": XattnConfig("xattn-tiny-fp32", 2, 37, 75, 64, 96, 2, 1, 32, "fp32", "layernorm", True, True, 1e-5, 22, 0.05),
 }
+
+
+@dataclass(frozen=True)
+class HeadConfig:
+    """The end of a model: a final norm, logits over the vocabulary, and their cross entropy with labels (top_k = 0) or with a
+    teacher's ``top_k`` top logits at a temperature.  ``tied``: the weights are stored [vocab, d_model], as an embedding is."""
+    name: str
+    batch: int
+    seq: int
+    d_model: int
+    vocab: int
+    dtype: str          # "fp32" or "bf16"
+    tied: bool
+    top_k: int
+    temperature: float
+    norm: str           # "layernorm" or "rmsnorm"
+    eps: float
+    seed: int
+    w_std: float
+
+    @property
+    def n_tokens(self) -> int:
+        return self.batch * self.seq
+
+    def flops(self) -> float:
+        """Algorithmic forward+backward flops: one product forward and two backward (the backward forms the logits once more)."""
+        return 3.0 * 2.0 * self.n_tokens * self.d_model * self.vocab

@@ -17,6 +17,7 @@ TENSOR_IDS = {
     "W1": 12, "Wg": 13, "W2": 14, "b1": 15, "bg": 16, "b2": 17,
     "Aq": 18, "Ak": 19, "Av": 20, "Bq": 21, "Bk": 22, "Bv": 23,
     "M": 24,
+    "W": 25, "targets": 26, "top_ids": 27, "top_logits": 28, "dloss": 29,
 }
 
 _M64 = np.uint64(0xFFFFFFFFFFFFFFFF)
@@ -172,4 +173,33 @@ def make_xattn_inputs(cfg, *, affine_noise: bool = False) -> dict:
         out["beta"] = np.zeros(d) if cfg.norm == "layernorm" else None
     for k, n in (("bq", dq), ("bk", dkv), ("bv", dkv), ("bo", d)):
         out[k] = vec(k, n, cfg.w_std) if cfg.has_bias else None
+    return out
+
+
+def make_head_inputs(cfg, *, ignored: float = 0.0, weighted: bool = False, affine_noise: bool = True) -> dict:
+    """All inputs of the head ``cfg`` (a ``HeadConfig``): X ~ N(0, 1) [batch, seq, d_model], W ~ N(0, w_std^2) ([vocab, d_model] if
+    tied), storage-rounded float64; norm gains; labels [batch, seq], or ids (distinct in a token) and logits [batch, seq, top_k] of a
+    teacher; about a share ``ignored`` of the tokens without a loss (labels of -100, or ids of -1); ``weighted``: per-token weights."""
+    s, n, d, v = cfg.seed, cfg.n_tokens, cfg.d_model, cfg.vocab
+    unit = lambda name, count: np.argsort(np.argsort(normal_f64(s, TENSOR_IDS[name], 0, count), kind="stable"), kind="stable") / max(count, 1)
+    w_shape = (v, d) if cfg.tied else (d, v)
+    out = {"X": round_to_storage(normal_f64(s, TENSOR_IDS["X"], 0, n * d).reshape(cfg.batch, cfg.seq, d), cfg.dtype),
+           "W": round_to_storage(normal_f64(s, TENSOR_IDS["W"], 0, d * v).reshape(w_shape) * cfg.w_std, cfg.dtype)}
+    vec = lambda name, mean: (normal_f64(s, TENSOR_IDS[name], 0, d) * (0.1 if affine_noise else 0.0) + mean).astype(np.float32).astype(np.float64)
+    out["gamma"], out["beta"] = vec("gamma", 1.0), vec("beta", 0.0) if cfg.norm == "layernorm" else None
+    if cfg.top_k:
+        k = cfg.top_k
+        start = (unit("targets", n) * v).astype(np.int64)
+        step = 1 + (unit("top_ids", n) * max(v // k - 1, 0)).astype(np.int64)           # distinct where k <= v
+        ids = (start[:, None] + step[:, None] * np.arange(k)[None, :]) % v
+        ids[unit("X", n) < ignored] = -1
+        out["top_ids"] = ids.reshape(cfg.batch, cfg.seq, k).astype(np.int32)
+        out["top_logits"] = (normal_f64(s, TENSOR_IDS["top_logits"], 0, n * k) * 2.0).astype(np.float32).astype(np.float64).reshape(cfg.batch, cfg.seq, k)
+    else:
+        t = np.minimum((unit("targets", n) * v).astype(np.int64), v - 1)
+        t[unit("X", n) < ignored] = -100
+        out["targets"] = t.reshape(cfg.batch, cfg.seq).astype(np.int32)
+    out["dloss"] = None
+    if weighted:
+        out["dloss"] = ((0.5 + unit("dloss", n)) / n).astype(np.float32).astype(np.float64).reshape(cfg.batch, cfg.seq)
     return out

@@ -406,6 +406,84 @@ int fbl_xattn_bwd(const fbl_plan* plan, const void* dY, const void* X, const voi
                   void* dWq, void* dWk, void* dWv, void* dWo, float* dbq, float* dbk, float* dbv, float* dbo,
                   float* dgamma, float* dbeta, void* scratch, void* stream);
 
+/* ---------------------------------------------------------------------------------------------------------------
+ * The norm as an operator of its own (the one behind the last layer, in front of the head): the layers' norm kernels on
+ * R-Tile matrices [batch, seq, d_model].
+ *   forward   Y = gamma (X - mean) rstd + beta (LayerNorm), Y = gamma X rstd with rstd of the mean square (RMSNorm)
+ *   backward  dX; dgamma = sum over the tokens of dY xhat, dbeta = sum of dY (fp32, two stages, no atomics: the same bits
+ *             every time).  dgamma and dbeta may both be NULL (the norm's parameters are frozen); dbeta is NULL for RMSNorm.
+ * `saved` carries (mean, rstd) of every padded token row; scratch_bwd holds the partial rows of the token-axis sums.
+ * Pointers, alignment, padding, streams and return codes as for the attention layer's calls.  gamma and beta are read before
+ * the launch in front has completed, as inputs of the step: no kernel of this library writes them. */
+typedef struct {
+  int32_t batch, seq, d_model;
+  int32_t dtype;        /* FBL_DTYPE_*  */
+  int32_t norm;         /* FBL_NORM_*   */
+  float eps;
+} fbl_norm_desc;
+typedef struct fbl_norm_plan fbl_norm_plan;
+int fbl_norm_plan_create(const fbl_norm_desc* desc, fbl_norm_plan** out);      /* d_model a multiple of tile_w, up to 16384 */
+void fbl_norm_plan_destroy(fbl_norm_plan* plan);
+int fbl_norm_tensor_bytes(const fbl_norm_plan* plan, size_t* bytes);           /* X, Y, dY, dX */
+int fbl_norm_workspace_bytes(const fbl_norm_plan* plan, size_t* saved, size_t* scratch_fwd, size_t* scratch_bwd);
+int fbl_norm_pack(const fbl_norm_plan* plan, const void* rowmajor_dev, void* tiled_dev, void* stream);
+int fbl_norm_unpack(const fbl_norm_plan* plan, const void* tiled_dev, void* rowmajor_dev, void* stream);
+int fbl_norm_fwd(const fbl_norm_plan* plan, const void* X, const float* gamma, const float* beta, void* Y, void* saved, void* scratch, void* stream);
+int fbl_norm_bwd(const fbl_norm_plan* plan, const void* dY, const void* X, const float* gamma, const void* saved, void* dX, float* dgamma,
+                 float* dbeta, void* scratch, void* stream);
+int64_t fbl_norm_launch_count(const fbl_norm_plan* plan);
+
+/* ---------------------------------------------------------------------------------------------------------------
+ * The head of a fine-tuning step: logits of the final hidden states over the vocabulary and their loss, forward and
+ * backward, a piece of the vocabulary at a time and without keeping the logits (128256 columns of 4096 tokens are 1 GB in
+ * bf16).  The products are the paper's reduce-axis-conflict operator once more (section 4.1); W, X and the logits' gradient
+ * stay in R-Tile order in both passes, transposes are operand-orientation flags.
+ *   logits        z = X W / temperature          (vocab_rows: z = X W^T / temperature)
+ *   target        y: 1 at the token's label; or the teacher's distribution, the softmax of its top_k logits / temperature
+ *                 over the ids given (ids given twice add up; nothing is assumed of the other ids, whose probability is 0)
+ *   loss          sum over v of y_v (log y_v - log softmax(z)_v) per token: cross entropy, or the Kullback-Leibler divergence
+ *   backward      dz = g (softmax(z) - y) / temperature, g the gradient of the token's loss;  dX = dz W^T;  dW = X^T dz
+ *
+ * Matrices: X [batch, seq, d_model] and dX; W and dW either [d_model, vocab], its columns padded to whole tiles with zeros, or,
+ * vocab_rows = 1, [vocab, d_model] (an embedding that is shared with the input side), its rows padded to eight with zeros.
+ * dW's padding comes back as zeros.  Any vocabulary from 1 to 2^20, top_k 0 (labels) to 128.
+ * Tokens without a loss: a label below zero (-100 is customary), or a teacher's list in which every id is below zero (entries
+ * with such ids are not there) or every logit -inf.  Their loss is 0, their rows of dX are 0 and they add nothing to dW,
+ * whatever their logits: the products run over the tokens with a loss only, and what the other rows of X hold is not looked at.
+ * A label or id of vocab or more, and a teacher's logit that is NaN or +inf, make the token's loss and row of dX NaN (and dW).
+ *
+ * loss [batch * seq] fp32; total[0] = sum of the losses, total[1] = number of tokens with a loss (device memory, both written).
+ * dloss [batch * seq] fp32, the gradient of each token's loss, or NULL: 1 / total[1], the gradient of the mean.  dX or dW may be
+ * NULL: then that gradient is not formed (a frozen head; a frozen model).  The backward reads the targets' entries and the
+ * softmax statistics from `saved`, and the X and W that the forward had; `saved` serves any number of backward calls.
+ * bf16 storage: products on bf16 operands with fp32 sums; statistics, losses and gradients in fp32, dz rounded to bf16 as an
+ * operand of the last two products.  The sums of dX over pieces and slices of the vocabulary are fp32, in a fixed order.
+ * FBL_HEAD_PIECE and FBL_HEAD_SLICES, read at plan creation, override the columns of a piece and the slices of dX's reduction
+ * (for tuning and tests only). */
+typedef struct {
+  int32_t batch, seq, d_model, vocab;
+  int32_t dtype;        /* FBL_DTYPE_*  */
+  int32_t vocab_rows;   /* 0: W is [d_model, vocab]; 1: [vocab, d_model] */
+  int32_t top_k;        /* 0: labels (fbl_head_xent_fwd); 1..128: a teacher's top logits (fbl_head_distill_fwd) */
+  float temperature;    /* > 0; 1 for labels */
+} fbl_head_desc;
+typedef struct fbl_head_plan fbl_head_plan;
+enum { FBL_HT_X = 0, FBL_HT_W, FBL_HT_COUNT };
+int fbl_head_plan_create(const fbl_head_desc* desc, fbl_head_plan** out);
+void fbl_head_plan_destroy(fbl_head_plan* plan);
+int fbl_head_tensor_bytes(const fbl_head_plan* plan, int matrix_id, size_t* bytes);
+int fbl_head_workspace_bytes(const fbl_head_plan* plan, size_t* saved, size_t* scratch_fwd, size_t* scratch_bwd);
+int fbl_head_pack(const fbl_head_plan* plan, int matrix_id, const void* rowmajor_dev, void* tiled_dev, void* stream);
+int fbl_head_unpack(const fbl_head_plan* plan, int matrix_id, const void* tiled_dev, void* rowmajor_dev, void* stream);
+int fbl_head_xent_fwd(const fbl_head_plan* plan, const void* X, const void* W, const int32_t* targets, float* loss, float* total,
+                      void* saved, void* scratch, void* stream);
+int fbl_head_distill_fwd(const fbl_head_plan* plan, const void* X, const void* W, const int32_t* top_ids, const float* top_logits,
+                         float* loss, float* total, void* saved, void* scratch, void* stream);
+int fbl_head_bwd(const fbl_head_plan* plan, const void* X, const void* W, const float* dloss, const void* saved, void* dX, void* dW,
+                 void* scratch, void* stream);
+int fbl_head_status_poll(const fbl_head_plan* plan, const void* scratch, int32_t* device_status);
+int64_t fbl_head_launch_count(const fbl_head_plan* plan);
+
 /* Kernel family used by later calls on this plan: 0 = default (tcgen05 tensor-core kernels for bf16 and, with operands in three bf16
  * parts, for fp32; FFMA kernels for fp32 attention of short sequences, of few memory rows or of heads of 128, for the attention
  * backward of bf16 layers with less than 128 token rows on either side, and for fp32 tiles with operands or results that are not finite

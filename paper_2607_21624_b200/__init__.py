@@ -9,8 +9,11 @@ from .binding import (FblError, Plan, lib, load_library, LayerRunner, DTYPES, TE
 
 from .lora import LoraRunner
 from .xattn import XattnRunner
+from .norm import NormPlan, NormRunner, norm_desc
+from .head import HeadPlan, HeadRunner, NormHeadRunner, head_desc, HEAD_TENSOR
 from .mlp import MlpPlan, MlpRunner, mlp_desc_from_config, MLP_TENSOR, MLP_WS
 
-__all__ = ["LoraRunner", "XattnRunner", "MlpPlan", "MlpRunner", "mlp_desc_from_config", "MLP_TENSOR", "MLP_WS",
+__all__ = ["NormPlan", "NormRunner", "norm_desc", "HeadPlan", "HeadRunner", "NormHeadRunner", "head_desc", "HEAD_TENSOR",
+           "LoraRunner", "XattnRunner", "MlpPlan", "MlpRunner", "mlp_desc_from_config", "MLP_TENSOR", "MLP_WS",
            "FblError", "Plan", "lib", "load_library", "LayerRunner", "DTYPES", "TENSOR", "MAP", "WS",
            "desc_from_config", "aligned_bytes", "guard_bands_intact", "selftest_wait_timeout"]

@@ -29,12 +29,15 @@ struct alignas(64) Problem {
   const float* b[MAX_TERMS];
   long long a_rpad[MAX_TERMS], b_rpad[MAX_TERMS];
   int k[MAX_TERMS];
+  int b_rows[MAX_TERMS];                    // stored rows of B
+  int dyn;                                  // 1: G.rows rows instead of m, 2: a reduction over G.rows (GemmArgs)
 };
 struct alignas(64) Group {
   Problem p[MAX_PROBLEMS];
   int from[MAX_PROBLEMS];                           // which of the caller's problems each is
   int count, slices, reset_status;
   int32_t* status;
+  const int32_t* rows;
   uint4* zero_ptr;                                  // chores of the launch, see GemmArgs
   long long zero_vec;
 };
@@ -55,7 +58,7 @@ inline bool fill_group(Group& G, const GemmArgs* gs, int count, const int* order
   for (int i = 0; i < count; ++i) {
     const GemmArgs& g = gs[G.from[i] = order[i]];
     Problem& P = G.p[i];
-    P.n_terms = g.n_terms; P.m = g.m; P.n = g.n; P.b_static = g.b_static;
+    P.n_terms = g.n_terms; P.m = g.c_rows ? (int)g.c_rows : g.m; P.n = g.n; P.b_static = g.b_static;
     for (int t = 0; t < g.n_terms; ++t) {
       const GemmTerm& tm = g.t[t];
       P.kblocks[t] = (tm.k + bk - 1) / bk;
@@ -63,17 +66,21 @@ inline bool fill_group(Group& G, const GemmArgs* gs, int count, const int* order
       P.a_k[t] = tm.a_trans ? 1 : 0;
       P.b_k[t] = tm.b_trans ? 0 : 1;
       P.a_rpad[t] = tm.a_rpad; P.b_rpad[t] = tm.b_rpad; P.k[t] = tm.k;
+      P.b_rows[t] = (int)(tm.b_rows ? tm.b_rows : tm.b_rpad);
       if (!fbl_encode_f32_rtile_map(&P.ta[t], tm.a, tm.a_rpad, (tm.a_trans ? g.m : tm.k) / 32, P.a_k[t] ? bk : bm, (P.a_k[t] ? bm : bk) / 32) ||
-          !fbl_encode_f32_rtile_map(&P.tb[t], tm.b, tm.b_rpad, (tm.b_trans ? tm.k : g.n) / 32, P.b_k[t] ? bk : bn, (P.b_k[t] ? bn : bk) / 32))
+          !fbl_encode_f32_rtile_map(&P.tb[t], tm.b, tm.b_rpad, (tm.b_trans ? tm.k : g.n) / 32, P.b_k[t] ? bk : bn, (P.b_k[t] ? bn : bk) / 32, tm.b_rows))
         return false;
     }
     P.tiles_m = (g.m + bm - 1) / bm; P.tiles_n = (g.n + bn - 1) / bn;
     P.c_rpad = g.c_rpad; P.seq = g.seq; P.t_pad = g.t_pad; P.dot_hd = g.dot_hd; P.dot_hq = g.dot_hq;
+    P.dyn = g.dyn;
+    if (g.dyn && (!g.rows || g.n_terms != 1 || g.rows != gs[0].rows)) return false;
   }
   return true;
 }
 inline bool point_group(Group& G, const GemmArgs* gs, int32_t* status) {
   G.status = status;
+  G.rows = gs[0].rows;
   G.zero_ptr = (uint4*)gs[0].zero_ptr; G.zero_vec = (long long)(gs[0].zero_bytes / 16); G.reset_status = gs[0].reset_status;
   bool ok = true;
   for (int i = 0; i < G.count; ++i) {

@@ -97,11 +97,29 @@ struct GemmTerm {
   const void* a; int64_t a_rpad; int a_trans;   // logical A[m,k]; a_trans: stored as [k rows][m cols]
   const void* b; int64_t b_rpad; int b_trans;   // logical B[k,n]; b_trans: stored as [n rows][k cols]
   int k;
+  int64_t b_rows;               // stored rows of B from its pointer on, where that is not the panels' start (0: b_rpad); zeros beyond
+};
+// The vocabulary epilogues of the head's products (head_epilogue.cuh).  A product's rows are the tokens that carry a loss, `row_of`
+// says which rows those are; what belongs to a row is at its own place.  A row's targets are entries, sorted by vocabulary id: ids and
+// probabilities at [entry][row], `count` of them (-1: the row's loss is NaN).
+struct HeadEpi {
+  const int32_t *ids, *count, *row_of;
+  const int32_t* n;             // how many rows have a loss, which may be none (GemmArgs.rows: at least 1)
+  const float* y;
+  long long rows;               // pitch of every per-row array here
+  int vocab, col0;              // columns of the vocabulary, and the first one of this product's
+  float scale;                  // from a product to a logit times log2 e
+  float2* part;                 // forward: [column tile][product's row] (k, sum of 2^(logit - k))
+  float* z_at;                  // forward: [entry][row] the products at the targets
+  const float *k, *sum;         // backward: the row's k and sum
+  const float* dloss;           // backward: the gradient of each token's loss [batch * seq], or else 1 (dX and dW are scaled)
+  float inv_tau;
 };
 struct GemmArgs {
   int m, n, n_terms;
   GemmTerm t[4];
   void* c; int64_t c_rpad;        // C[m,n] stored [m rows][n cols]
+  int64_t c_rows;                 // rows of C that are stored, where fewer than m (0: m)
   const float* bias;              // per output column, or nullptr
   const void* residual;           // same layout as C, or nullptr
   int seq, t_pad;                 // if t_pad > 0: rows with (row % t_pad) >= seq are written as zero
@@ -111,6 +129,14 @@ struct GemmArgs {
   // reduction loop cut into ksplit slices whose fp32 partial tiles are added into `acc` (zeroed by the caller, same
   // element order as C with 4-byte elements); the norm backward rounds them to C (ConvertGroup)
   int ksplit; float* acc;
+  // instead: ksplit slices (one will do) with an area each in `acc`, stored (acc_mode 1) or added to what it holds (2), so that
+  // the order of additions is the launches' own; whoever launches adds the areas up (own_slices: how many there are)
+  int acc_mode;
+  const float* over;              // C = alpha / max(*over, 1) times the product, where not null (rounded products without epilogue extras)
+  float alpha;
+  // how many rows there are to a product whose rows (dyn 1) or reduction (dyn 2) are the tokens that carry a loss: a number of m, or
+  // k, and at least 1, that only the device knows (one address for the whole group)
+  const int32_t* rows; int dyn;
   // of a group's first problem: chores of the launch (zero-fill zero_bytes, a multiple of 16, at zero_ptr for a
   // later kernel of the pass; reset the pass's status word), and `serial`: the launch may not start before
   // everything ahead of it on the stream has completed
@@ -123,7 +149,9 @@ struct GemmArgs {
   // 2 GELU backward (c = value * gelu'(U), U in `residual`), 3 gated forward (c = G, c2 = silu(G) * U, U in `residual`),
   // 4 gated backward (c = value * silu(G), c2 = value * U * silu'(G); U in `residual`, G in `aux1`)
   // 5 rotary embedding of heads of 64 columns, with the table launch_norm_fwd leaves (see there)
+  // 6 softmax statistics of the vocabulary's logits (no C), 7 the gradient of their cross entropy: `head`
   int epi; const void* aux1; void* c2; const float2* rope;
+  HeadEpi head;
 };
 
 cudaError_t launch_gemm_simt(const GemmArgs& g, cudaStream_t st);
@@ -161,6 +189,9 @@ static inline bool rope_in_projection(const fbl_plan* p, GemmArgs* gs, const flo
 __host__ __device__ __forceinline__ int gemm_slice_begin(int total, int slices, int slice) { return total * slice / slices; }
 struct GemmShape { int64_t m; int n; int kblocks; int splittable; };
 int gemm_tc_choose_split(int sm_count, const GemmShape* sh, int count, bool zero_rides);
+// The same for slices with areas of their own, of the group's last problem.
+int gemm_tc_choose_own_slices(int sm_count, const GemmShape* sh, int count);
+constexpr int HEAD_TILE = 256;      // columns of a partial of the softmax statistics
 cudaError_t launch_wait_timeout_selftest(int32_t* status, long long limit_cycles, cudaStream_t st);
 // With less than a tile of token rows on either side a bf16 layer keeps P and dS in fp32, or in two bf16 values: their rounding
 // is as large as that of the results there (dQ, dK, dV off by 2.3e-3 of their norm instead of 1.65e-3), and with the rotary

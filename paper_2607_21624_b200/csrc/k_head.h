@@ -1,0 +1,37 @@
+// Launchers of the kernels around the head's products (k_head.cu).
+#pragma once
+#include "fbl_internal.h"
+
+constexpr int HEAD_MAX_TOP = 128;       // teacher logits a token
+constexpr int HEAD_TICKET = 32;         // word of the status word's block in which head_combine_kernel counts its blocks
+namespace headk { constexpr int NONE = 0x7fffffff; }
+
+// What the forward keeps of the padded token rows, in `saved`.  The products run over the rows that carry a loss, in their order.
+struct HeadRows {
+  int64_t rows;
+  int32_t *ids, *count;       // entries, see HeadEpi (count 0: no loss)
+  int32_t *row_of, *pos;      // the products' rows' token rows, and the other way round (-1: none)
+  int32_t* n;                 // [2] rows with a loss, the same and at least 1
+  float *y, *constant;        // constant: sum of y log y
+  float *k, *sum;             // softmax statistics
+  float* total;               // [2] loss, counted tokens
+};
+
+// Labels, or what teacher_entries has left in `count`, to positions; rows of X with a loss to Xc, zeros behind them to whole tiles.
+cudaError_t launch_head_rows(int dtype, const int32_t* targets, const HeadRows& R, int seq, int t_pad, int vocab, const void* X, void* Xc, int d_model,
+                             int32_t* status, cudaStream_t st);
+cudaError_t launch_teacher_entries(const int32_t* ids, const float* logits, int top_k, float temperature, const HeadRows& R, int seq, int t_pad,
+                                   int vocab, int32_t* status, cudaStream_t st);
+// The rows of X with a loss again (their positions are known); starts a pass.
+cudaError_t launch_head_gather(int dtype, const HeadRows& R, const void* X, void* Xc, int d_model, int32_t* status, cudaStream_t st);
+cudaError_t launch_head_combine(const float2* part, int tiles, const float* z_at, const HeadRows& R, float scale, float* loss, float* total,
+                                float* block_sums, int seq, int t_pad, int32_t* status, cudaStream_t st);
+cudaError_t launch_head_stats_f32(const float* z, const HeadRows& R, int vocab, int col0, int cols, float scale, float2* part, float* z_at,
+                                  cudaStream_t st);
+cudaError_t launch_head_grad_f32(float* z, const HeadRows& R, const float* dloss, int vocab, int col0, int cols, float scale, float inv_tau, int seq,
+                                 int t_pad, cudaStream_t st);
+// dX from the areas' sums, times alpha / max(*over, 1) where `over` is not null
+cudaError_t launch_head_scatter(int dtype, int sm_count, const float* acc, int areas, const HeadRows& R, int d_model, const float* over, float alpha,
+                                void* dX, cudaStream_t st);
+// [rows][cols] <-> tiles of [rows][padded], for a number of columns that is not whole tiles
+cudaError_t launch_pack_columns(int dtype, int unpack, const void* src, void* dst, int64_t rows, int cols, int padded, cudaStream_t st);

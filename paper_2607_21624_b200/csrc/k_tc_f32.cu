@@ -98,7 +98,7 @@ __device__ __noinline__ void plain_tile(const Problem& P, uint32_t tile, uint32_
     for (int k0 = kb * BK; k0 < min(kb * BK + BK, P.k[t]); k0 += KS) {
       __syncthreads();
       fill(sa, LDA, BM, P.a[t], P.a_rpad[t], P.a_k[t] != 0, m0, P.m, k0, P.k[t]);
-      fill(sb, LDB, BN, P.b[t], P.b_rpad[t], P.b_k[t] != 0, n0, P.n, k0, P.k[t]);
+      fill(sb, LDB, BN, P.b[t], P.b_rpad[t], P.b_k[t] != 0, n0, P.b_k[t] ? P.n : min(P.n, P.b_rows[t]), k0, P.b_k[t] ? min(P.k[t], P.b_rows[t]) : P.k[t]);
       __syncthreads();
       if (threadIdx.x < GROUPS) {
 #pragma unroll 4
@@ -140,6 +140,19 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_tc_f32_kernel(const __grid_co
   auto added = [&](int b) { return bars + 8u * (2 * STAGES + 4 + b); };     // the accumulator has been read
   const int warp = (int)tc::uniform(threadIdx.x / 32), lane = threadIdx.x % 32;
   const tc::Status status(G.status, G.reset_status);
+  // work unit: (problem, tile, slice); the slices of a tile are the blocks of a cluster
+  const int slice = blockIdx.x % G.slices;
+  int w = blockIdx.x / G.slices, pi = 0;
+  while (w >= G.p[pi].tiles_m * G.p[pi].tiles_n) { w -= G.p[pi].tiles_m * G.p[pi].tiles_n; ++pi; }
+  const Problem& P = G.p[pi];
+  const int m0 = (w % P.tiles_m) * BM, n0 = (w / P.tiles_m) * BN;
+  int total_kb = P.total_kb;
+  if (P.dyn) {                               // fewer rows, or less to reduce, than the launch was made for
+    pdl_wait();
+    const int rows = __ldcg(G.rows);
+    if (P.dyn == 1 && m0 >= rows) return;      // all blocks of a cluster alike
+    if (P.dyn == 2) total_kb = (rows + BK - 1) / BK;
+  }
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) {
       tc::mbar_init(full(s), 1);
@@ -164,13 +177,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_tc_f32_kernel(const __grid_co
   asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem_base) : "r"(slot));
   tmem_base = tc::uniform(tmem_base);
   pdl_launch_dependents();
-  // work unit: (problem, tile, slice); the slices of a tile are the blocks of a cluster
-  const int slice = blockIdx.x % G.slices;
-  int w = blockIdx.x / G.slices, pi = 0;
-  while (w >= G.p[pi].tiles_m * G.p[pi].tiles_n) { w -= G.p[pi].tiles_m * G.p[pi].tiles_n; ++pi; }
-  const Problem& P = G.p[pi];
-  const int m0 = (w % P.tiles_m) * BM, n0 = (w / P.tiles_m) * BN;
-  const int kb_begin = gemm_slice_begin(P.total_kb, G.slices, slice), n_kb = gemm_slice_begin(P.total_kb, G.slices, slice + 1) - kb_begin;
+  const int kb_begin = gemm_slice_begin(total_kb, G.slices, slice), n_kb = gemm_slice_begin(total_kb, G.slices, slice + 1) - kb_begin;
 
   if (warp == 0) {
     if (lane == 0) {

@@ -10,6 +10,7 @@
 #include <mutex>
 
 #include "fbl_internal.h"
+#include "head_epilogue.cuh"
 #include "launch_memo.h"
 #include "pdl.cuh"
 #include "tc_common.cuh"
@@ -40,11 +41,17 @@ struct alignas(64) TcProblem {
   // later kernel rounds the sums to bf16.  Single-term problems without epilogue extras only.
   int ksplit;
   CUtensorMap tacc;
+  int sums, slice_panels;          // sums: 0 rounded to C, 1 stored, 2 added to tacc's buffer; slice_panels: from one slice's area to the next
+  HeadEpi head;
+  int dyn;                         // 1: G.rows rows instead of m, 2: a reduction over G.rows
+  const float* over;               // C = alpha / max(*over, 1) times the product, where not null
+  float alpha;
   // Fused activation of the feed-forward block (kernel variant EPI only; `residual` then points at the first extra
   // operand U instead of a residual, `aux1` at the second one, G; `tc2` is the second output's map):
   //   1 GELU forward    C = v (U), C2 = gelu(v)           2 GELU backward    C = v gelu'(U)
   //   3 gated forward   C = v (G), C2 = silu(v) U          4 gated backward   C = v silu(G), C2 = v U silu'(G)
   //   5 rotary embedding C = v with each 64-column head's (i, i + 32) pairs turned by the table's angle of the row's token
+  //   6, 7 (kernel variants of their own) the vocabulary's softmax, head_epilogue.cuh
   const float2* rope;      // [32][t_pad] cosine and sine
   int epi;
   const __nv_bfloat16* aux1;
@@ -56,6 +63,8 @@ struct alignas(64) TcGroup {
   int late_trigger;                          // as in GemmArgs: the dependents' trigger comes after the wait
   int slices;                                // gemm_tc_split_kernel: blocks of a cluster, which share a tile's reduction
   int32_t* status;
+  const int32_t* rows;                       // see GemmArgs
+  int dynamic;                               // 1: the work list depends on it
   // Optional chores for the epilogue warps while the first tile's main loop runs: zero-fill a buffer that a later
   // kernel of the pass adds into (16-byte units, dealt evenly to the blocks), and reset the pass's status word.
   uint4* zero_ptr;
@@ -92,22 +101,33 @@ struct SmemPlan {
 
 // Work list of a launch: output tiles of all problems, numbered problem by problem with the M tile index
 // fastest (blocks that run together then share the B tiles of one weight column block through L2).
-struct TileCoord { int prob, m0, n0, kb0, kb1; };     // kb0..kb1: k-block range of term 0 (split problems)
+struct TileCoord { int prob, m0, n0, kb0, kb1, slice; };     // kb0..kb1: k-block range of term 0 (split problems)
+
+// `rows`: the device's number of rows, for problems that go by it.
+__device__ __forceinline__ int rows_of(const TcProblem& P, int rows) { return P.dyn == 1 ? rows : P.m; }
+__device__ __forceinline__ int kblocks_of(const TcProblem& P, int rows) { return P.dyn == 2 ? (rows + BK - 1) / BK : P.kblocks[0]; }
+// Before a role's first look at the work list.
+__device__ __forceinline__ int dynamic_rows(const TcGroup& G) {
+  if (!G.dynamic) return 0;
+  pdl_wait();
+  return __ldcg(G.rows);
+}
 
 template <int BN>
-__device__ __forceinline__ bool tile_at(const TcGroup& G, int w, TileCoord* tc_out) {
+__device__ __forceinline__ bool tile_at(const TcGroup& G, int rows, int w, TileCoord* tc_out) {
   for (int p = 0; p < G.count; ++p) {
     const TcProblem& P = G.p[p];
-    const int tm = (P.m + BM - 1) / BM, tn = (P.n + BN - 1) / BN;
+    const int tm = (rows_of(P, rows) + BM - 1) / BM, tn = (P.n + BN - 1) / BN;
     const int units = tm * tn * P.ksplit;
     if (w < units) {
       const int slice = w % P.ksplit, t = w / P.ksplit;        // slices of one tile are neighbours in the list
       tc_out->prob = p;
       tc_out->m0 = (t % tm) * BM;
       tc_out->n0 = (t / tm) * BN;
-      const int per = (P.kblocks[0] + P.ksplit - 1) / P.ksplit;
+      const int kb = kblocks_of(P, rows), per = (kb + P.ksplit - 1) / P.ksplit;
+      tc_out->slice = slice;
       tc_out->kb0 = slice * per;
-      tc_out->kb1 = min(P.kblocks[0], (slice + 1) * per);
+      tc_out->kb1 = min(kb, (slice + 1) * per);
       return true;
     }
     w -= units;
@@ -142,9 +162,9 @@ struct TmemAcc {
 // warps share the tile's 64-column panels, first and second half, and the epilogue takes half as long.  Each warp then
 // has one staging tile instead of two (the staging area is the same size).
 // EPI: what the instantiation can fuse besides bias, residual and the row reduction.
-enum { EPI_NONE = 0, EPI_ACT, EPI_ROPE };
+enum { EPI_NONE = 0, EPI_ACT, EPI_ROPE, EPI_HEAD_STATS, EPI_HEAD_GRAD };
 template <int BN, int ESETS, int EPI, typename Acc, typename Wait>
-__device__ __forceinline__ bool epilogue_tile(const TcProblem& P, int m0, int n0, int q, Acc acc, uint32_t stg0, int& pc, Wait wait) {
+__device__ __forceinline__ bool epilogue_tile(const TcProblem& P, int m0, int n0, int slice, int q, Acc acc, uint32_t stg0, int& pc, Wait wait) {
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, set = (warp - 2) / 4;
   constexpr int PPS = BN / 64 / ESETS;              // panels per set
   const int row = m0 + q * 32 + lane;               // row of the problem owned by this thread
@@ -189,9 +209,9 @@ __device__ __forceinline__ bool epilogue_tile(const TcProblem& P, int m0, int n0
     acc.load(pn * 64, *reinterpret_cast<uint32_t(*)[32]>(&v[0]));
     acc.load(pn * 64 + 32, *reinterpret_cast<uint32_t(*)[32]>(&v[32]));
     acc.wait();
-    if (P.ksplit > 1) {
+    if (P.sums) {
       // partial sums of a reduction slice: two 32-column halves of the panel, fp32, added to the accumulation
-      // buffer by bulk tensor reductions (same staging tiles and swizzle as the bf16 rows below)
+      // buffer by bulk tensor reductions, or stored there (same staging tiles and swizzle as the bf16 rows below)
 #pragma unroll 1
       for (int hf = 0; hf < 2; ++hf) {
         const uint32_t stg = stg0 + (ESETS == 2 ? (uint32_t)(warp - 2) : (uint32_t)(q * 2 + (pc & 1))) * 4096u;
@@ -205,7 +225,9 @@ __device__ __forceinline__ bool epilogue_tile(const TcProblem& P, int m0, int n0
         tc::fence_proxy_async();
         __syncwarp();
         if (lane == 0) {
-          tc::tma_reduce_add_4d(&P.tacc, stg, 0, hf, m0 + q * 32, n / 64);
+          const int panel = n / 64 + slice * P.slice_panels;
+          if (P.sums == 1) tc::tma_store_4d(&P.tacc, stg, 0, hf, m0 + q * 32, panel);
+          else tc::tma_reduce_add_4d(&P.tacc, stg, 0, hf, m0 + q * 32, panel);
           tc::bulk_commit_group();
           if (ESETS == 1) tc::bulk_wait_group_read1();
         }
@@ -299,6 +321,13 @@ __device__ __forceinline__ bool epilogue_tile(const TcProblem& P, int m0, int n0
         continue;
       }
     }
+    if constexpr (EPI == EPI_NONE) {
+      if (P.over) {
+        const float a = P.alpha / fmaxf(*P.over, 1.f);
+#pragma unroll
+        for (int j = 0; j < 64; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * a);
+      }
+    }
     bool bias_left = bias != nullptr;
     if constexpr (EPI == EPI_ROPE) {
       if (P.epi == 5) {
@@ -390,6 +419,14 @@ __device__ __forceinline__ bool epilogue_tile(const TcProblem& P, int m0, int n0
   return true;
 }
 
+// The epilogue that an instantiation has.
+template <int BN, int ESETS, int EPI, typename Acc, typename Wait>
+__device__ __forceinline__ bool fused_epilogue_tile(const TcProblem& P, int m0, int n0, int slice, int q, Acc acc, uint32_t stg0, int& pc, Wait wait) {
+  if constexpr (EPI == EPI_HEAD_STATS) return head_stats_tile<BN>(P, m0, n0, q, acc, wait);
+  else if constexpr (EPI == EPI_HEAD_GRAD) return head_grad_tile<BN>(P, m0, n0, q, acc, stg0, pc, wait);
+  else return epilogue_tile<BN, ESETS, EPI>(P, m0, n0, slice, q, acc, stg0, pc, wait);
+}
+
 // Persistent kernel: one block per SM walks the work list with stride gridDim.x.  Warp 0 feeds the
 // shared-memory ring by TMA, warp 1 issues the MMAs into one of two TMEM accumulators, warps 2-5 drain the
 // other accumulator (bias, residual, padding-row mask, bf16 rows in R-Tile order), so the epilogue of
@@ -446,7 +483,8 @@ __global__ void __maxnreg__(ESETS == 2 ? 168 : EPI == EPI_ACT ? 255 : 224) gemm_
     // Weights do not depend on the kernel before this one: their tiles for the first stages of the first
     // output tile are requested before waiting for that kernel, hiding their (cold) latency.
     int prefilled = 0;
-    if (tile_at<BN>(G, blockIdx.x, &tcd) && G.p[tcd.prob].b_static && G.p[tcd.prob].ksplit == 1) {
+    const int rows = dynamic_rows(G);
+    if (tile_at<BN>(G, rows, blockIdx.x, &tcd) && G.p[tcd.prob].b_static && G.p[tcd.prob].ksplit == 1) {
       const TcProblem& P = G.p[tcd.prob];
       if (leader) { tc::tma_prefetch_desc(&P.ta[0]); tc::tma_prefetch_desc(&P.tb[0]); }
       const int n = P.kblocks[0] < STAGES ? P.kblocks[0] : STAGES;
@@ -461,7 +499,7 @@ __global__ void __maxnreg__(ESETS == 2 ? 168 : EPI == EPI_ACT ? 255 : 224) gemm_
     }
     pdl_wait();
     if (G.late_trigger && leader) late_trigger(G);
-    for (int w = blockIdx.x; ok && tile_at<BN>(G, w, &tcd); w += gridDim.x) {
+    for (int w = blockIdx.x; ok && tile_at<BN>(G, rows, w, &tcd); w += gridDim.x) {
       const TcProblem& P = G.p[tcd.prob];
       for (int t = 0; t < P.n_terms && ok; ++t) {
         int kb = t == 0 ? tcd.kb0 : 0;
@@ -500,7 +538,8 @@ __global__ void __maxnreg__(ESETS == 2 ? 168 : EPI == EPI_ACT ? 255 : 224) gemm_
     bool ok = true;
     TileCoord tcd;
     const uint32_t hi = tc::smem_desc_hi(1024);
-    for (int w = blockIdx.x; ok && tile_at<BN>(G, w, &tcd); w += gridDim.x, ++ti) {
+    const int rows = dynamic_rows(G);
+    for (int w = blockIdx.x; ok && tile_at<BN>(G, rows, w, &tcd); w += gridDim.x, ++ti) {
       const TcProblem& P = G.p[tcd.prob];
       const int ab = ti & 1;
       if (!tc::mbar_wait_warp(acc_empty(ab), ((ti >> 1) & 1) ^ 1, status, 104)) { ok = false; break; }
@@ -535,13 +574,14 @@ __global__ void __maxnreg__(ESETS == 2 ? 168 : EPI == EPI_ACT ? 255 : 224) gemm_
     pdl_wait();                                       // the previous kernel may still be reading what we overwrite
     group_chores(G, threadIdx.x - 64, 128 * ESETS);
     const int q = warp % 4;                           // the TMEM lane quarter this warp may access
+    const int rows = dynamic_rows(G);
     int ti = 0, pc = 0;                               // tiles and panels done by this warp
     bool ok = true;
     TileCoord tcd;
-    for (int w = blockIdx.x; ok && tile_at<BN>(G, w, &tcd); w += gridDim.x, ++ti) {
+    for (int w = blockIdx.x; ok && tile_at<BN>(G, rows, w, &tcd); w += gridDim.x, ++ti) {
       const TcProblem& P = G.p[tcd.prob];
       const int ab = ti & 1;
-      const bool ready = epilogue_tile<BN, ESETS, EPI>(P, tcd.m0, tcd.n0, q, TmemAcc{tmem_base + ((uint32_t)(q * 32) << 16) + ab * BN}, base + SP::STG_OFF, pc, [&] {
+      const bool ready = fused_epilogue_tile<BN, ESETS, EPI>(P, tcd.m0, tcd.n0, tcd.slice, q, TmemAcc{tmem_base + ((uint32_t)(q * 32) << 16) + ab * BN}, base + SP::STG_OFF, pc, [&] {
         return tc::mbar_wait(acc_full(ab), (ti >> 1) & 1, status, 103);
       });
       if (!ready) { ok = false; break; }
@@ -578,10 +618,10 @@ struct PairSmem {
 // L2 holds (8192 x 4096 attention step: 5060 -> 4945 us, its four product launches 535, 172, 378, 1191 -> 505, 167, 364, 1131; bands
 // of 16 the same).  Up to 16 row tiles fit as they are (4096 x 2048 x 8192 feed-forward in bands of eight: 88 -> 92 us a launch).
 constexpr int PAIR_BAND = 8, PAIR_BAND_FROM = 16;
-__device__ __forceinline__ bool pair_tile_at(const TcGroup& G, int w, TileCoord* tc_out) {
+__device__ __forceinline__ bool pair_tile_at(const TcGroup& G, int rows, int w, TileCoord* tc_out) {
   for (int p = 0; p < G.count; ++p) {
     const TcProblem& P = G.p[p];
-    const int tm = (P.m + 255) / 256, tn = (P.n + 255) / 256;
+    const int tm = (rows_of(P, rows) + 255) / 256, tn = (P.n + 255) / 256;
     const int units = tm * tn * P.ksplit;
     if (w < units) {
       const int slice = w % P.ksplit, t = w / P.ksplit;
@@ -589,9 +629,10 @@ __device__ __forceinline__ bool pair_tile_at(const TcGroup& G, int w, TileCoord*
       const int band = tm > PAIR_BAND_FROM ? PAIR_BAND : tm, at = t / (band * tn), h = min(band, tm - at * band), u = t - at * band * tn;
       tc_out->m0 = (at * band + u % h) * 256;
       tc_out->n0 = (u / h) * 256;
-      const int per = (P.kblocks[0] + P.ksplit - 1) / P.ksplit;
+      const int kb = kblocks_of(P, rows), per = (kb + P.ksplit - 1) / P.ksplit;
+      tc_out->slice = slice;
       tc_out->kb0 = slice * per;
-      tc_out->kb1 = min(P.kblocks[0], (slice + 1) * per);
+      tc_out->kb1 = min(kb, (slice + 1) * per);
       return true;
     }
     w -= units;
@@ -651,7 +692,8 @@ __global__ void __cluster_dims__(2, 1, 1) __maxnreg__(EPI == EPI_ACT ? 255 : 224
     const uint32_t full0 = tc::map_to_cta(full(0), 0);
     pdl_wait();
     if (G.late_trigger && leader) late_trigger(G);
-    for (int w = pair_id; ok && pair_tile_at(G, w, &tcd); w += n_pairs) {
+    const int rows = dynamic_rows(G);
+    for (int w = pair_id; ok && pair_tile_at(G, rows, w, &tcd); w += n_pairs) {
       const TcProblem& P = G.p[tcd.prob];
       const int m0 = tcd.m0 + (int)rank * 128, n0 = tcd.n0 + (int)rank * 128;
       for (int t = 0; t < P.n_terms && ok; ++t) {
@@ -682,7 +724,8 @@ __global__ void __cluster_dims__(2, 1, 1) __maxnreg__(EPI == EPI_ACT ? 255 : 224
     bool ok = true;
     TileCoord tcd;
     const uint32_t hi = tc::smem_desc_hi(1024);
-    for (int w = pair_id; ok && pair_tile_at(G, w, &tcd); w += n_pairs, ++ti) {
+    const int rows = dynamic_rows(G);
+    for (int w = pair_id; ok && pair_tile_at(G, rows, w, &tcd); w += n_pairs, ++ti) {
       const TcProblem& P = G.p[tcd.prob];
       const int ab = ti & 1;
       if (!tc::mbar_wait_warp(acc_empty(ab), ((ti >> 1) & 1) ^ 1, status, 114)) { ok = false; break; }
@@ -715,14 +758,15 @@ __global__ void __cluster_dims__(2, 1, 1) __maxnreg__(EPI == EPI_ACT ? 255 : 224
     pdl_wait();
     group_chores(G, threadIdx.x - 64, 128);
     const int q = warp % 4;
+    const int rows = dynamic_rows(G);
     int ti = 0, pc = 0;
     bool ok = true;
     TileCoord tcd;
-    for (int w = pair_id; ok && pair_tile_at(G, w, &tcd); w += n_pairs, ++ti) {
+    for (int w = pair_id; ok && pair_tile_at(G, rows, w, &tcd); w += n_pairs, ++ti) {
       const TcProblem& P = G.p[tcd.prob];
       const int ab = ti & 1;
       const int m0 = tcd.m0 + (int)rank * 128;
-      const bool ready = epilogue_tile<BN, 1, EPI>(P, m0, tcd.n0, q, TmemAcc{tmem_base + ((uint32_t)(q * 32) << 16) + ab * BN}, base + SP::STG_OFF, pc, [&] {
+      const bool ready = fused_epilogue_tile<BN, 1, EPI>(P, m0, tcd.n0, tcd.slice, q, TmemAcc{tmem_base + ((uint32_t)(q * 32) << 16) + ab * BN}, base + SP::STG_OFF, pc, [&] {
         return tc::mbar_wait(acc_full(ab), (ti >> 1) & 1, status, 113);
       });
       if (!ready) { ok = false; break; }
@@ -798,7 +842,7 @@ __global__ void __launch_bounds__(320, 1) gemm_tc_split_kernel(const __grid_cons
 
   const int slice = blockIdx.x % G.slices;
   TileCoord tcd;
-  tile_at<BN>(G, blockIdx.x / G.slices, &tcd);
+  tile_at<BN>(G, 0, blockIdx.x / G.slices, &tcd);
   const TcProblem& P = G.p[tcd.prob];
   int total = 0;
   for (int t = 0; t < P.n_terms; ++t) total += P.kblocks[t];
@@ -917,7 +961,7 @@ __global__ void __launch_bounds__(320, 1) gemm_tc_split_kernel(const __grid_cons
     const int rg = slice * groups + q;                   // the row group this warp finishes (the first `groups` warps of a set)
     int pc = 0;
     if (q < groups && tcd.m0 + rg * 32 < P.m)
-      epilogue_tile<BN, 2, EPI>(P, tcd.m0, tcd.n0, rg, PartialAcc{base + (rg * 32 + lane) * SPLIT_LD * 4}, base + SP::STG_OFF, pc, exchange);
+      epilogue_tile<BN, 2, EPI>(P, tcd.m0, tcd.n0, 0, rg, PartialAcc{base + (rg * 32 + lane) * SPLIT_LD * 4}, base + SP::STG_OFF, pc, exchange);
     else
       exchange();
     if (lane == 0) tc::bulk_wait_group0();
@@ -988,10 +1032,10 @@ bool fbl_map_set_base(CUtensorMap* map, const void* base) {
 }
 
 static bool encode_panels(CUtensorMap* map, CUtensorMapDataType type, int width, const void* base, int64_t r_pad, int panels,
-                          int box_rows, int box_panels) {
+                          int box_rows, int box_panels, int64_t rows) {
   EncodeTiledFn fn = encode_fn();
   if (!fn) return false;
-  cuuint64_t dims[3] = {(cuuint64_t)width, (cuuint64_t)r_pad, (cuuint64_t)panels};
+  cuuint64_t dims[3] = {(cuuint64_t)width, (cuuint64_t)(rows ? rows : r_pad), (cuuint64_t)panels};
   cuuint64_t strides[2] = {128, (cuuint64_t)r_pad * 128};
   cuuint32_t box[3] = {(cuuint32_t)width, (cuuint32_t)box_rows, (cuuint32_t)box_panels};
   cuuint32_t estr[3] = {1, 1, 1};
@@ -1013,11 +1057,11 @@ bool fbl_encode_seq_map(CUtensorMap* map, bool f32, const void* base, int rows, 
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-bool fbl_encode_rtile_map(CUtensorMap* map, const void* base, int64_t r_pad, int panels, int box_rows, int box_panels) {
-  return encode_panels(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 64, base, r_pad, panels, box_rows, box_panels);
+bool fbl_encode_rtile_map(CUtensorMap* map, const void* base, int64_t r_pad, int panels, int box_rows, int box_panels, int64_t rows) {
+  return encode_panels(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 64, base, r_pad, panels, box_rows, box_panels, rows);
 }
-bool fbl_encode_f32_rtile_map(CUtensorMap* map, const void* base, int64_t r_pad, int panels, int box_rows, int box_panels) {
-  return encode_panels(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 32, base, r_pad, panels, box_rows, box_panels);
+bool fbl_encode_f32_rtile_map(CUtensorMap* map, const void* base, int64_t r_pad, int panels, int box_rows, int box_panels, int64_t rows) {
+  return encode_panels(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 32, base, r_pad, panels, box_rows, box_panels, rows);
 }
 
 // fp32 accumulator [n_pad, cols] stored in the bf16 tile order (64-column panels, 256-byte rows), viewed as
@@ -1073,16 +1117,23 @@ cudaError_t fill_group(TcGroup& G, const GemmArgs* gs, int count, int bn_box, in
       if (tm.a_trans) ok = fbl_encode_rtile_map(&P.ta[t], tm.a, tm.a_rpad, g.m / 64, BK, BM / 64);
       else ok = fbl_encode_rtile_map(&P.ta[t], tm.a, tm.a_rpad, tm.k / 64, BM, 1);
       if (!ok) return cudaErrorInvalidValue;
-      if (tm.b_trans) ok = fbl_encode_rtile_map(&P.tb[t], tm.b, tm.b_rpad, tm.k / 64, bn_box, 1);
-      else ok = fbl_encode_rtile_map(&P.tb[t], tm.b, tm.b_rpad, g.n / 64, BK, bn_box / 64);
+      if (tm.b_trans) ok = fbl_encode_rtile_map(&P.tb[t], tm.b, tm.b_rpad, tm.k / 64, bn_box, 1, tm.b_rows);
+      else ok = fbl_encode_rtile_map(&P.tb[t], tm.b, tm.b_rpad, g.n / 64, BK, bn_box / 64, tm.b_rows);
       if (!ok) return cudaErrorInvalidValue;
     }
     P.m = g.m; P.n = g.n;
-    if (!fbl_encode_rtile_map(&P.tc, g.c, g.c_rpad, g.n / 64, 32, 1)) return cudaErrorInvalidValue;   // one warp's rows
+    if (g.epi != 6 && !fbl_encode_rtile_map(&P.tc, g.c, g.c_rpad, g.n / 64, 32, 1, g.c_rows)) return cudaErrorInvalidValue;   // one warp's rows
+    // with rows enough for one tile at most, the work list is known without the device's number
+    P.dyn = g.dyn == 1 && g.m <= tile_m ? 0 : g.dyn;
+    G.dynamic |= P.dyn;
+    if (g.dyn && (!g.rows || g.n_terms != 1 || g.rows != gs[0].rows || (g.dyn == 2 && g.ksplit > 1))) return cudaErrorInvalidValue;
     P.b_static = g.b_static;
     P.c_rpad = g.c_rpad; P.seq = g.seq; P.t_pad = g.t_pad;
     P.dot_hd = g.dot_hd; P.dot_hq = g.dot_hq; P.epi = g.epi;
-    if (g.epi != 0) {
+    if (g.epi >= 6) {
+      if (g.epi > 7 || g.ksplit > 1 || g.acc_mode || g.n_terms != 1 || g.bias || g.residual || g.dot_with || !g.head.ids || !g.head.count || !g.head.row_of || !g.head.n || !g.rows)
+        return cudaErrorInvalidValue;
+    } else if (g.epi != 0) {
       const bool rope = g.epi == 5, two_out = g.epi != 2 && !rope;
       if (g.epi < 1 || g.epi > 5 || g.ksplit > 1 || g.dot_with || (g.epi >= 2 && !rope && !g.residual) || (g.epi == 4 && !g.aux1) ||
           (two_out && !g.c2) || (rope && (!g.rope || g.residual || g.t_pad <= 0)))
@@ -1090,11 +1141,13 @@ cudaError_t fill_group(TcGroup& G, const GemmArgs* gs, int count, int bn_box, in
       if (two_out && !fbl_encode_rtile_map(&P.tc2, g.c2, g.c_rpad, g.n / 64, 32, 1)) return cudaErrorInvalidValue;
     }
     P.ksplit = 1;
-    if (g.ksplit > 1) {
+    if (g.ksplit > 1 || g.acc_mode) {
       if (g.n_terms != 1 || g.bias || g.residual || g.dot_with || g.t_pad > 0 || !g.acc) return cudaErrorInvalidValue;
-      const int per = (P.kblocks[0] + g.ksplit - 1) / g.ksplit;        // no empty slice
+      const int slices = g.ksplit > 1 ? g.ksplit : 1, per = (P.kblocks[0] + slices - 1) / slices;        // no empty slice
       P.ksplit = (P.kblocks[0] + per - 1) / per;
-      if (!fbl_encode_f32_panel_map(&P.tacc, g.acc, g.c_rpad, g.n / 64, 32, 1)) return cudaErrorInvalidValue;
+      P.sums = g.acc_mode == 1 ? 1 : 2;
+      P.slice_panels = g.acc_mode ? g.n / 64 : 0;
+      if (!fbl_encode_f32_panel_map(&P.tacc, g.acc, g.c_rpad, g.acc_mode ? g.n / 64 * P.ksplit : g.n / 64, 32, 1)) return cudaErrorInvalidValue;
     }
     tiles += ((g.m + tile_m - 1) / tile_m) * ((g.n + tile_n - 1) / tile_n) * P.ksplit;
   }
@@ -1108,7 +1161,7 @@ namespace {
 int group_epi(const GemmArgs* gs, int count) {
   int epi = EPI_NONE;
   for (int i = 0; i < count; ++i)
-    if (gs[i].epi != 0) epi = gs[i].epi == 5 ? EPI_ROPE : EPI_ACT;
+    if (gs[i].epi != 0) epi = gs[i].epi == 5 ? EPI_ROPE : gs[i].epi == 6 ? EPI_HEAD_STATS : gs[i].epi == 7 ? EPI_HEAD_GRAD : EPI_ACT;
   return epi;
 }
 
@@ -1131,15 +1184,18 @@ cudaError_t group_launch(GroupLaunch& L, void (*k)(const TcGroup), int grid, int
 bool point_group(GroupLaunch& L, const GemmArgs* gs, int32_t* status) {
   TcGroup& G = L.G;
   G.status = status;
+  G.rows = gs[0].rows;
   G.zero_ptr = (uint4*)gs[0].zero_ptr; G.zero_vec = (long long)(gs[0].zero_bytes / 16); G.reset_status = gs[0].reset_status;
   bool ok = true;
   for (int i = 0; i < G.count; ++i) {
     const GemmArgs& g = gs[L.order[i]];
     TcProblem& P = G.p[i];
     for (int t = 0; t < P.n_terms; ++t) ok = ok && fbl_map_set_base(&P.ta[t], g.t[t].a) && fbl_map_set_base(&P.tb[t], g.t[t].b);
-    ok = ok && fbl_map_set_base(&P.tc, g.c);
-    if (P.epi != 0 && P.epi != 2 && P.epi != 5) ok = ok && fbl_map_set_base(&P.tc2, g.c2);
-    if (P.ksplit > 1 || g.ksplit > 1) ok = ok && fbl_map_set_base(&P.tacc, g.acc);
+    if (P.epi != 6) ok = ok && fbl_map_set_base(&P.tc, g.c);
+    if (P.epi != 0 && P.epi != 2 && P.epi < 5) ok = ok && fbl_map_set_base(&P.tc2, g.c2);
+    if (P.sums) ok = ok && fbl_map_set_base(&P.tacc, g.acc);
+    P.head = g.head;
+    P.over = g.over; P.alpha = g.alpha;
     P.c = (__nv_bfloat16*)g.c; P.bias = g.bias; P.residual = (const __nv_bfloat16*)g.residual;
     P.dot_with = (const __nv_bfloat16*)g.dot_with; P.dot_out = g.dot_out;
     P.aux1 = (const __nv_bfloat16*)g.aux1; P.rope = g.rope;
@@ -1165,6 +1221,21 @@ cudaError_t make_group_bn(GroupLaunch& L, const fbl_plan* p, const GemmArgs* gs,
     default: k = two_sets ? gemm_tc_kernel<BN, STAGES, SETS, EPI_NONE> : gemm_tc_kernel<BN, STAGES, 1, EPI_NONE>;
   }
   return group_launch(L, k, grid, two_sets ? 320 : 192, SmemPlan<BN, STAGES>::TOTAL, gs[0].serial);
+}
+
+// The head's products: 256 columns to a tile (a partial of the softmax statistics is a tile's), on one CTA or a pair.
+cudaError_t make_group_head(GroupLaunch& L, const fbl_plan* p, const GemmArgs* gs, int count, bool pair) {
+  int tiles = 0;
+  if (count != 1) return cudaErrorInvalidValue;
+  const bool stats = gs[0].epi == 6;
+  cudaError_t e = fill_group(L.G, gs, count, pair ? 128 : 256, pair ? 256 : BM, 256, &tiles);
+  if (e != cudaSuccess) return e;
+  if (pair) {
+    const int pairs = tiles < p->sm_count / 2 ? tiles : p->sm_count / 2;
+    return group_launch(L, stats ? gemm_tc_pair_kernel<EPI_HEAD_STATS> : gemm_tc_pair_kernel<EPI_HEAD_GRAD>, 2 * pairs, 192, PairSmem::TOTAL, gs[0].serial);
+  }
+  return group_launch(L, stats ? gemm_tc_kernel<256, 4, 1, EPI_HEAD_STATS> : gemm_tc_kernel<256, 4, 1, EPI_HEAD_GRAD>,
+                      tiles < p->sm_count ? tiles : p->sm_count, 192, SmemPlan<256, 4>::TOTAL, gs[0].serial);
 }
 
 cudaError_t make_group_split(GroupLaunch& L, const GemmArgs* gs, int count, int slices) {
@@ -1289,6 +1360,10 @@ static cudaError_t make_group(GroupLaunch& L, const fbl_plan* p, const GemmArgs*
     w[i] = {gs[i].m, gs[i].n, 0, gs[i].ksplit > 1 ? gs[i].ksplit : 1};
     for (int t = 0; t < gs[i].n_terms; ++t) w[i].kb += (gs[i].t[t].k + BK - 1) / BK;
   }
+  if (gs[0].epi >= 6) {
+    const double one = tile_makespan(TILE_COST[TILE_WIDE], w, count, p->sm_count), two = tile_makespan(TILE_COST[TILE_PAIR], w, count, p->sm_count / 2);
+    return make_group_head(L, p, gs, count, pair_mode >= 0 ? pair_mode == 1 : two < one);
+  }
   if (pair_mode == 1) {
     kind = TILE_PAIR;
   } else if (ch.bn) {
@@ -1300,7 +1375,7 @@ static cudaError_t make_group(GroupLaunch& L, const fbl_plan* p, const GemmArgs*
       const double t = tile_makespan(TILE_COST[TILE_SLIM], w, count, p->sm_count);
       if (t < clocks) { clocks = t; kind = TILE_SLIM; }
     }
-    const int slices = best_slices(w, count, p->sm_count, clocks);
+    const int slices = gs[0].rows ? 0 : best_slices(w, count, p->sm_count, clocks);       // (a slice needs a k-block)
     if (slices) {
       L.idle = 1 << 20;                              // fewer blocks than SMs, as a rule
       return make_group_split(L, gs, count, slices);
@@ -1378,4 +1453,22 @@ int gemm_tc_choose_split(int sm_count, const GemmShape* sh, int count, bool zero
     else if (cost < (zero_rides ? 0.9 : 0.85) * base_cost && cost < best_cost) { best = S; best_cost = cost; }   // worth it only with a clear gain
   }
   return best;
+}
+
+int gemm_tc_choose_own_slices(int sm_count, const GemmShape* sh, int count) {
+  static const int cand[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+  double best_cost = 1e300;
+  int best = 1;
+  for (int S : cand) {
+    if (S > 1 && sh[count - 1].kblocks / S < 8) break;
+    TileWork w[MAX_PROBLEMS];
+    for (int i = 0; i < count; ++i) w[i] = {sh[i].m, sh[i].n, sh[i].kblocks, i == count - 1 ? S : 1};
+    double cost;
+    best_tile(w, count, sm_count, true, &cost);
+    // the areas are written once and read once, at some 3400 bytes a clock
+    cost += (double)S * sh[count - 1].m * sh[count - 1].n * 8 / 3400;
+    if (cost < (S == 1 ? 1.0 : 0.97) * best_cost) { best = S; best_cost = cost; }
+  }
+  const int per = (sh[count - 1].kblocks + best - 1) / best;                  // no empty slice
+  return (sh[count - 1].kblocks + per - 1) / per;
 }

@@ -120,6 +120,11 @@ __device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, uint32_t sr
                ::"l"((uint64_t)map), "r"(src), "r"(x), "r"(y), "r"(z)
                : "memory");
 }
+__device__ __forceinline__ void tma_store_4d(const CUtensorMap* map, uint32_t src, int c0, int c1, int c2, int c3) {
+  asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5}], [%1];"
+               ::"l"((uint64_t)map), "r"(src), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
+               : "memory");
+}
 __device__ __forceinline__ void bulk_wait_group_read1() { asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory"); }
 __device__ __forceinline__ void bulk_commit_group() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void bulk_wait_group_read0() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
@@ -403,10 +408,11 @@ __device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap
 
 }  // namespace tc
 
-// Host side: encode a 3-D tensor map over an R-Tile bf16 matrix viewed as [panels][rows][64].
+// Host side: encode a 3-D tensor map over an R-Tile bf16 matrix viewed as [panels][rows][64].  `rows`: of the map, where it is
+// not r_pad (a matrix seen from one of its rows on).
 bool fbl_map_set_base(CUtensorMap* map, const void* base);      // an encoded map at another address
-bool fbl_encode_rtile_map(CUtensorMap* map, const void* base, int64_t r_pad, int panels, int box_rows, int box_panels);
-bool fbl_encode_f32_rtile_map(CUtensorMap* map, const void* base, int64_t r_pad, int panels, int box_rows, int box_panels);   // fp32: [panels][rows][32]
+bool fbl_encode_rtile_map(CUtensorMap* map, const void* base, int64_t r_pad, int panels, int box_rows, int box_panels, int64_t rows = 0);
+bool fbl_encode_f32_rtile_map(CUtensorMap* map, const void* base, int64_t r_pad, int panels, int box_rows, int box_panels, int64_t rows = 0);   // fp32: [panels][rows][32]
 // A matrix of `seqs` sequences of `rows` rows each, seen as [panels][seqs][rows][128 bytes]: a box that reaches past its sequence's
 // rows is filled with zeros, not with the next sequence's values (which, not finite, would pass a weight of zero).
 bool fbl_encode_seq_map(CUtensorMap* map, bool f32, const void* base, int rows, int seqs, int panels, int box_rows, int box_panels);
