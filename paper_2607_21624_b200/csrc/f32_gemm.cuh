@@ -30,6 +30,10 @@ struct alignas(64) Problem {
   long long a_rpad[MAX_TERMS], b_rpad[MAX_TERMS];
   int k[MAX_TERMS];
   int b_rows[MAX_TERMS];                    // stored rows of B
+  // the reduction cut into `areas` ranges, work units of their own, whose sums go to a copy of C each, area_stride floats apart
+  int areas;
+  long long area_stride;
+  HeadEpi head;                             // of the vocabulary's products (epilogues 6 and 7)
   int dyn;                                  // 1: G.rows rows instead of m, 2: a reduction over G.rows (GemmArgs)
 };
 struct alignas(64) Group {
@@ -44,7 +48,7 @@ struct alignas(64) Group {
 
 // Problems in the order of their reductions' lengths: the blocks that take longest start first.
 inline void longest_first(const GemmArgs* gs, int count, int* order) {
-  auto length = [&](int i) { long long k = 0; for (int t = 0; t < gs[i].n_terms; ++t) k += gs[i].t[t].k; return k; };
+  auto length = [&](int i) { long long k = 0; for (int t = 0; t < gs[i].n_terms; ++t) k += gs[i].t[t].k; return gs[i].acc_mode && gs[i].ksplit > 1 ? k / gs[i].ksplit : k; };
   for (int i = 0; i < count; ++i) {
     int j = i;
     for (; j > 0 && length(order[j - 1]) < length(i); --j) order[j] = order[j - 1];
@@ -73,6 +77,8 @@ inline bool fill_group(Group& G, const GemmArgs* gs, int count, const int* order
     }
     P.tiles_m = (g.m + bm - 1) / bm; P.tiles_n = (g.n + bn - 1) / bn;
     P.c_rpad = g.c_rpad; P.seq = g.seq; P.t_pad = g.t_pad; P.dot_hd = g.dot_hd; P.dot_hq = g.dot_hq;
+    P.areas = g.acc_mode && g.ksplit > 1 ? g.ksplit : 1;
+    P.area_stride = g.c_rpad * g.n;
     P.dyn = g.dyn;
     if (g.dyn && (!g.rows || g.n_terms != 1 || g.rows != gs[0].rows)) return false;
   }
@@ -90,19 +96,21 @@ inline bool point_group(Group& G, const GemmArgs* gs, int32_t* status) {
       ok = ok && fbl_map_set_base(&P.ta[t], g.t[t].a) && fbl_map_set_base(&P.tb[t], g.t[t].b);
       P.a[t] = (const float*)g.t[t].a; P.b[t] = (const float*)g.t[t].b;
     }
-    P.c = (float*)g.c; P.bias = g.bias; P.residual = (const float*)g.residual;
+    P.c = g.acc_mode ? g.acc : (float*)g.c; P.bias = g.bias; P.residual = g.acc_mode == 2 ? g.acc : (const float*)g.residual;
     P.dot_with = (const float*)g.dot_with; P.dot_out = g.dot_out;
+    P.head = g.head;
   }
   return ok;
 }
 
 using tc::lds4;
 
+// (`area`: where the unit's copy of C begins.)
 // This block's share of the tile's rows: the slices' sums (each block's at `base` of its shared memory, rows LD floats apart)
 // in slice order, bias, residual, padding rows, 16-byte stores.  A thread keeps its four columns and has two rows in flight (one
 // at a time, each waiting for its loads, an 800 x 768 x 768 product took 2 us longer).
 template <int BM, int BN, int LD, int THREADS>
-__device__ __forceinline__ void finish_tile(const Problem& P, int slices, int slice, uint32_t base, int m0, int n0) {
+__device__ __forceinline__ void finish_tile(const Problem& P, int slices, int slice, uint32_t base, int m0, int n0, int64_t area = 0) {
   constexpr int VECS = BN / 4, STEP = THREADS / VECS, U = 2;
   static_assert(THREADS % VECS == 0, "whole rows");
   const int rows = BM / slices, r0 = slice * rows;
@@ -118,7 +126,7 @@ __device__ __forceinline__ void finish_tile(const Problem& P, int slices, int sl
       live[u] = i < rows && m < P.m && n < P.n;
       s[u] = extra[u] = make_float4(0.f, 0.f, 0.f, 0.f);
       if (!live[u]) continue;
-      const int64_t off = rt_off<32>(P.c_rpad, m, n);
+      const int64_t off = area + rt_off<32>(P.c_rpad, m, n);
       if (P.residual) extra[u] = *reinterpret_cast<const float4*>(P.residual + off);
       else if (P.dot_with) extra[u] = *reinterpret_cast<const float4*>(P.dot_with + off);
     }
@@ -146,9 +154,9 @@ __device__ __forceinline__ void finish_tile(const Problem& P, int slices, int sl
       if (live[u]) {
         float4 v = s[u];
         v.x += bias.x; v.y += bias.y; v.z += bias.z; v.w += bias.w;
-        const int64_t off = rt_off<32>(P.c_rpad, m, n);
+        const int64_t off = area + rt_off<32>(P.c_rpad, m, n);
         if (P.residual) { v.x += extra[u].x; v.y += extra[u].y; v.z += extra[u].z; v.w += extra[u].w; }
-        if (P.t_pad > 0 && m % P.t_pad >= P.seq) v = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (P.t_pad > 0 && !P.dyn && m % P.t_pad >= P.seq) v = make_float4(0.f, 0.f, 0.f, 0.f);
         *reinterpret_cast<float4*>(P.c + off) = v;
         if (P.dot_with) {
           const float4 q = P.residual ? *reinterpret_cast<const float4*>(P.dot_with + off) : extra[u];

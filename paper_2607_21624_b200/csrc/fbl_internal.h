@@ -109,10 +109,11 @@ struct HeadEpi {
   long long rows;               // pitch of every per-row array here
   int vocab, col0;              // columns of the vocabulary, and the first one of this product's
   float scale;                  // from a product to a logit times log2 e
-  float2* part;                 // forward: [column tile][product's row] (k, sum of 2^(logit - k))
+  float2* part;                 // forward: [product's row][column tile, `tiles` of them] (k, sum of 2^(logit - k))
+  int tiles;
   float* z_at;                  // forward: [entry][row] the products at the targets
   const float *k, *sum;         // backward: the row's k and sum
-  const float* dloss;           // backward: the gradient of each token's loss [batch * seq], or else 1 (dX and dW are scaled)
+  const float *dloss, *over;    // backward: the gradient of each token's loss [batch * seq], or else 1 / max(*over, 1), or else 1
   float inv_tau;
 };
 struct GemmArgs {
@@ -130,7 +131,7 @@ struct GemmArgs {
   // element order as C with 4-byte elements); the norm backward rounds them to C (ConvertGroup)
   int ksplit; float* acc;
   // instead: ksplit slices (one will do) with an area each in `acc`, stored (acc_mode 1) or added to what it holds (2), so that
-  // the order of additions is the launches' own; whoever launches adds the areas up (own_slices: how many there are)
+  // the order of additions is the launches' own; whoever launches adds the areas up.  bf16 and fp32
   int acc_mode;
   const float* over;              // C = alpha / max(*over, 1) times the product, where not null (rounded products without epilogue extras)
   float alpha;
@@ -189,9 +190,11 @@ static inline bool rope_in_projection(const fbl_plan* p, GemmArgs* gs, const flo
 __host__ __device__ __forceinline__ int gemm_slice_begin(int total, int slices, int slice) { return total * slice / slices; }
 struct GemmShape { int64_t m; int n; int kblocks; int splittable; };
 int gemm_tc_choose_split(int sm_count, const GemmShape* sh, int count, bool zero_rides);
-// The same for slices with areas of their own, of the group's last problem.
-int gemm_tc_choose_own_slices(int sm_count, const GemmShape* sh, int count);
-constexpr int HEAD_TILE = 256;      // columns of a partial of the softmax statistics
+// The same for slices with areas of their own, of dX beside dW (which may be null).
+int gemm_tc_choose_own_slices(int sm_count, const GemmShape* dw, const GemmShape& dx);
+// Areas of an fp32 group's last problem, whose other fields but addresses are set.
+int gemm_tc_f32_choose_areas(const fbl_plan* p, GemmArgs* gs, int count);
+constexpr int HEAD_TILE = 256, HEAD_TILE_F32 = 64;      // columns of a partial of the softmax statistics
 cudaError_t launch_wait_timeout_selftest(int32_t* status, long long limit_cycles, cudaStream_t st);
 // With less than a tile of token rows on either side a bf16 layer keeps P and dS in fp32, or in two bf16 values: their rounding
 // is as large as that of the results there (dQ, dK, dV off by 2.3e-3 of their norm instead of 1.65e-3), and with the rotary

@@ -1,8 +1,7 @@
 // The head of a fine-tuning step: logits X W over the vocabulary and their softmax cross entropy with labels, or with a teacher's
 // top logits, a piece of the vocabulary at a time and without keeping a logit; and the norm in front of it as a plan of its own.
-// bf16: the forward is one product whose epilogue keeps softmax statistics; the backward forms a piece's logits again, leaves
+// The forward is one product whose epilogue keeps softmax statistics; the backward forms a piece's logits again, leaves
 // their gradient dz from the same epilogue (head_epilogue.cuh), and feeds it to dX += dz W^T and dW = X^T dz in one launch.
-// fp32: the same with the logits of a piece in memory between the product and a pass over them.
 #include <math.h>
 #include <stdlib.h>
 
@@ -36,9 +35,16 @@ int base_plan(int batch, int seq, int d_model, int dtype, int norm, float eps, f
   return fbl_plan_create(&ld, out);
 }
 
-// A piece's logits or their gradient take up to this much scratch.  Every piece adds dX up once more (8 bytes an element), so
-// pieces should be large; nothing else depends on their size.
-constexpr int64_t PIECE_BYTES = (int64_t)256 << 20;
+// Columns of a piece.  Its logits' gradient is written once and read twice by the two products behind, so it had better stay in L2:
+// 8192 x 4096 over 32000 columns 6201 us a step with 128 MB, 6368 with 256 MB, 6280 with one piece, 6458 with 32 MB (the power cap
+// is what is felt there).  But each piece costs two launches' start and end, some 10 us: pieces of less than half a Tflop are up to
+// 256 MB (2048 x 768 over 50257 columns 348 us in one piece of 206 MB, 361 in two).
+int64_t piece_columns(int64_t n_pad, int d_model, int e) {
+  int64_t piece = ((int64_t)128 << 20) / (n_pad * e);
+  const int64_t enough = (int64_t)(0.5e12 / (6.0 * (double)n_pad * d_model));
+  if (piece < enough) piece = enough < 2 * piece ? enough : 2 * piece;
+  return piece > 2048 ? piece / HEAD_TILE * HEAD_TILE : 2048;
+}
 
 // The tensor core's additions round toward zero, so that a logit comes out smaller in magnitude: by 2.2e-8 of itself and 1.62e-8 more
 // for each 16 columns where the terms have one sign (2.1e-6 at 2048 columns, 4.2e-6 at 4096: logits of tokens that the hidden state
@@ -57,9 +63,9 @@ struct fbl_head_plan {
   int top_k, tiles;             // entries a row; partials of the softmax statistics
   int piece, pieces, slices;    // columns of a piece; pieces; areas that dX's reduction is cut into
   float scale;                  // from a product to a logit times log2 e
-  size_t sv_ids, sv_y, sv_count, sv_constant, sv_row_of, sv_pos, sv_n, sv_k, sv_sum, sv_total, saved_bytes;
-  size_t sf_x, sf_part, sf_z, sf_blocks, sf_logits, scratch_fwd_bytes;
-  size_t sb_x, sb_dz, sb_acc, scratch_bwd_bytes;
+  size_t sv_ids, sv_y, sv_count, sv_constant, sv_row_of, sv_pos, sv_n, sv_k, sv_sum, sv_total, sv_x, saved_bytes;
+  size_t sf_part, sf_z, sf_blocks, scratch_fwd_bytes;
+  size_t sb_dz, sb_acc, scratch_bwd_bytes;
   mutable int64_t launches;
 };
 struct fbl_norm_plan {
@@ -79,6 +85,7 @@ HeadRows rows_of(const fbl_head_plan* p, const void* saved) {
   R.row_of = (int32_t*)(sv + p->sv_row_of); R.pos = (int32_t*)(sv + p->sv_pos); R.n = (int32_t*)(sv + p->sv_n);
   R.k = (float*)(sv + p->sv_k); R.sum = (float*)(sv + p->sv_sum);
   R.total = (float*)(sv + p->sv_total);
+  R.x = sv + p->sv_x;
   return R;
 }
 
@@ -102,14 +109,37 @@ int64_t piece_rows(const fbl_head_plan* p, int col0, int cols) {
   return p->d.vocab_rows ? (left < cols ? left : cols) : 0;
 }
 
+// The products behind a piece of dz but for addresses: a token-axis reduction, dz^T X [vocab, d_model] or X^T dz, and dz W^T.
+GemmArgs dw_product(const fbl_head_plan* p, int cols) {
+  GemmArgs g = {};
+  const int n = (int)p->n_pad, D = p->d.d_model;
+  g.dyn = 2;
+  g.n_terms = 1;
+  if (p->d.vocab_rows) { g.m = cols; g.n = D; }
+  else { g.m = D; g.n = cols; }
+  g.t[0] = {nullptr, p->n_pad, 1, nullptr, p->n_pad, 0, n, 0};
+  g.c_rpad = p->w_rows;
+  return g;
+}
+GemmArgs dx_product(const fbl_head_plan* p, int cols) {
+  GemmArgs g = {};
+  g.dyn = 1;
+  g.n_terms = 1;
+  g.m = (int)p->n_pad; g.n = p->d.d_model;
+  g.t[0] = {nullptr, p->n_pad, 0, nullptr, p->w_rows, p->d.vocab_rows ? 0 : 1, cols, 0};
+  g.c_rpad = p->n_pad;
+  return g;
+}
+
 // Logits of columns col0 .. col0 + cols - 1: X [tokens with a loss, d_model] times W's piece.
-GemmArgs logits_product(const fbl_head_plan* p, const HeadRows& R, const void* X, const void* W, int col0, int cols) {
+GemmArgs logits_product(const fbl_head_plan* p, const HeadRows& R, const void* W, int col0, int cols) {
   GemmArgs g = {};
   g.rows = R.n + 1; g.dyn = 1;
   g.m = (int)p->n_pad; g.n = cols; g.n_terms = 1;
-  g.t[0] = {X, p->n_pad, 0, weights_at(p, W, col0), p->w_rows, p->d.vocab_rows, p->d.d_model, piece_rows(p, col0, cols)};
+  g.t[0] = {R.x, p->n_pad, 0, weights_at(p, W, col0), p->w_rows, p->d.vocab_rows, p->d.d_model, piece_rows(p, col0, cols)};
   g.b_static = 1;
   g.c_rpad = p->n_pad;
+  g.seq = p->d.seq; g.t_pad = p->base->t_pad;
   return g;
 }
 
@@ -121,27 +151,15 @@ int run_products(const fbl_head_plan* p, GemmArgs* gs, int count, int32_t* statu
 }
 #define HEAD_RUN(expr) do { const int rc__ = (expr); if (rc__ != FBL_OK) return rc__; } while (0)
 
-int forward(const fbl_head_plan* p, const void* Xc, const void* W, float* loss, float* total, const HeadRows& R, char* sf, cudaStream_t st) {
+int forward(const fbl_head_plan* p, const void* W, float* loss, float* total, const HeadRows& R, char* sf, cudaStream_t st) {
   int32_t* status = (int32_t*)sf;
   float2* part = (float2*)(sf + p->sf_part);
   float* z_at = (float*)(sf + p->sf_z);
-  if (p->d.dtype == FBL_DTYPE_BF16) {
-    GemmArgs g = logits_product(p, R, Xc, W, 0, p->cols);
-    g.epi = 6;
-    g.head = epilogue_of(p, R, 0);
-    g.head.part = part; g.head.z_at = z_at;
-    g.seq = p->d.seq; g.t_pad = p->base->t_pad;
-    HEAD_RUN(run_products(p, &g, 1, status, st));
-  } else {
-    float* z = (float*)(sf + p->sf_logits);
-    for (int col0 = 0; col0 < p->cols; col0 += p->piece) {
-      const int cols = p->cols - col0 < p->piece ? p->cols - col0 : p->piece;
-      GemmArgs g = logits_product(p, R, Xc, W, col0, cols);
-      g.c = z;
-      HEAD_RUN(run_products(p, &g, 1, status, st));
-      HEAD_STEP(launch_head_stats_f32(z, R, p->d.vocab, col0, cols, p->scale, part, z_at, st));
-    }
-  }
+  GemmArgs g = logits_product(p, R, W, 0, p->cols);
+  g.epi = 6;
+  g.head = epilogue_of(p, R, 0);
+  g.head.part = part; g.head.tiles = p->tiles; g.head.z_at = z_at;
+  HEAD_RUN(run_products(p, &g, 1, status, st));
   HEAD_STEP(launch_head_combine(part, p->tiles, z_at, R, p->scale, loss, total, (float*)(sf + p->sf_blocks), p->d.seq, p->base->t_pad, status, st));
   return FBL_OK;
 }
@@ -174,12 +192,11 @@ int fbl_head_plan_create(const fbl_head_desc* desc, fbl_head_plan** out) {
   p->cols = (int)up(d.vocab, base->tw);
   p->w_rows = d.vocab_rows ? up(d.vocab, 8) : d.d_model;
   p->top_k = d.top_k ? d.top_k : 1;
-  p->tiles = (p->cols + HEAD_TILE - 1) / HEAD_TILE;
+  p->tiles = bf16 ? (p->cols + HEAD_TILE - 1) / HEAD_TILE : (p->cols + HEAD_TILE_F32 - 1) / HEAD_TILE_F32;
   p->scale = (float)(1.4426950408889634 / (double)d.temperature * (1.0 + (bf16 ? logit_lift(d.d_model) : 0.0)));
 
   // pieces of about one size, in whole tiles
-  const int64_t most = PIECE_BYTES / (p->n_pad * base->e) / HEAD_TILE * HEAD_TILE;
-  int64_t piece = most > 2048 ? most : 2048;
+  int64_t piece = piece_columns(p->n_pad, d.d_model, base->e);
   if (getenv("FBL_HEAD_PIECE") && atoi(getenv("FBL_HEAD_PIECE")) > 0) piece = up(atoi(getenv("FBL_HEAD_PIECE")), HEAD_TILE);   // tuning / test knob
   p->pieces = (int)((p->cols + piece - 1) / piece);
   p->piece = (int)up((p->cols + p->pieces - 1) / p->pieces, HEAD_TILE);
@@ -187,15 +204,19 @@ int fbl_head_plan_create(const fbl_head_desc* desc, fbl_head_plan** out) {
   if (p->piece > p->cols) p->piece = p->cols;
 
   // dX reduces over a piece of the vocabulary, beside dW, which reduces over the tokens: cut the former where it balances the SMs
-  p->slices = 1;
-  if (bf16) {
-    const GemmShape dw = {d.vocab_rows ? p->piece : d.d_model, d.vocab_rows ? d.d_model : p->piece, (int)((p->n_pad + 63) / 64), 0};
-    const GemmShape sh[2] = {dw, {p->n_pad, d.d_model, (p->piece + 63) / 64, 1}};
-    p->slices = gemm_tc_choose_own_slices(base->sm_count, sh, 2);
-    if (getenv("FBL_HEAD_SLICES") && atoi(getenv("FBL_HEAD_SLICES")) > 0) {                                                   // likewise
-      const int kb = (p->piece + 63) / 64, want = atoi(getenv("FBL_HEAD_SLICES")), per = (kb + want - 1) / want;
-      p->slices = (kb + per - 1) / per;
+  {
+    GemmArgs gs[2] = {dw_product(p, p->piece), dx_product(p, p->piece)};
+    const int kb = (p->piece + 63) / 64;
+    int want = 1;
+    if (bf16) {
+      const GemmShape dw = {gs[0].m, gs[0].n, (gs[0].t[0].k + 63) / 64, 0};
+      want = gemm_tc_choose_own_slices(base->sm_count, &dw, {gs[1].m, gs[1].n, kb, 1});
+    } else {
+      want = gemm_tc_f32_choose_areas(base, gs, 2);
     }
+    if (getenv("FBL_HEAD_SLICES") && atoi(getenv("FBL_HEAD_SLICES")) > 0) want = atoi(getenv("FBL_HEAD_SLICES"));               // likewise
+    const int per = (kb + want - 1) / want;                                                                                   // none empty
+    p->slices = (kb + per - 1) / per;
   }
 
   const size_t n = (size_t)p->n_pad;
@@ -211,18 +232,15 @@ int fbl_head_plan_create(const fbl_head_desc* desc, fbl_head_plan** out) {
   p->sv_k = take(o, n * 4);
   p->sv_sum = take(o, n * 4);
   p->sv_total = take(o, 8);
+  p->sv_x = take(o, n * d.d_model * base->e);
   p->saved_bytes = o;
   const size_t piece_bytes = n * p->piece * base->e;
   o = FBL_ALIGN;                // status word
-  p->sf_x = take(o, n * d.d_model * base->e);
   p->sf_part = take(o, n * p->tiles * sizeof(float2));
   p->sf_z = take(o, n * p->top_k * 4);
   p->sf_blocks = take(o, n / 8 * 8);
-  p->sf_logits = o;
-  if (!bf16) (void)take(o, piece_bytes);
   p->scratch_fwd_bytes = o;
   o = FBL_ALIGN;
-  p->sb_x = take(o, n * d.d_model * base->e);
   p->sb_dz = take(o, piece_bytes);
   p->sb_acc = take(o, n * d.d_model * 4 * p->slices);
   p->scratch_bwd_bytes = o;
@@ -296,8 +314,8 @@ int fbl_head_xent_fwd(const fbl_head_plan* p, const void* X, const void* W, cons
   cudaStream_t st = as_stream(stream);
   const HeadRows R = rows_of(p, saved);
   char* sf = (char*)scratch;
-  HEAD_STEP(launch_head_rows(p->d.dtype, targets, R, p->d.seq, p->base->t_pad, p->d.vocab, X, sf + p->sf_x, p->d.d_model, (int32_t*)sf, st));
-  return forward(p, sf + p->sf_x, W, loss, total, R, sf, st);
+  HEAD_STEP(launch_head_rows(p->d.dtype, targets, R, p->d.seq, p->base->t_pad, p->d.vocab, X, p->d.d_model, (int32_t*)sf, st));
+  return forward(p, W, loss, total, R, sf, st);
 }
 
 int fbl_head_distill_fwd(const fbl_head_plan* p, const void* X, const void* W, const int32_t* top_ids, const float* top_logits, float* loss,
@@ -309,8 +327,8 @@ int fbl_head_distill_fwd(const fbl_head_plan* p, const void* X, const void* W, c
   const HeadRows R = rows_of(p, saved);
   char* sf = (char*)scratch;
   HEAD_STEP(launch_teacher_entries(top_ids, top_logits, p->d.top_k, p->d.temperature, R, p->d.seq, p->base->t_pad, p->d.vocab, (int32_t*)sf, st));
-  HEAD_STEP(launch_head_rows(p->d.dtype, nullptr, R, p->d.seq, p->base->t_pad, p->d.vocab, X, sf + p->sf_x, p->d.d_model, (int32_t*)sf, st));
-  return forward(p, sf + p->sf_x, W, loss, total, R, sf, st);
+  HEAD_STEP(launch_head_rows(p->d.dtype, nullptr, R, p->d.seq, p->base->t_pad, p->d.vocab, X, p->d.d_model, (int32_t*)sf, st));
+  return forward(p, W, loss, total, R, sf, st);
 }
 
 int fbl_head_bwd(const fbl_head_plan* p, const void* X, const void* W, const float* dloss, const void* saved, void* dX, void* dW, void* scratch,
@@ -322,57 +340,44 @@ int fbl_head_bwd(const fbl_head_plan* p, const void* X, const void* W, const flo
   const HeadRows R = rows_of(p, saved);
   char* sc = (char*)scratch;
   int32_t* status = (int32_t*)sc;
-  void *Xc = sc + p->sb_x, *dz = sc + p->sb_dz;
+  void* dz = sc + p->sb_dz;
   float* acc = (float*)(sc + p->sb_acc);
   const bool bf16 = p->d.dtype == FBL_DTYPE_BF16;
-  const int n = (int)p->n_pad, D = p->d.d_model;
+  const int D = p->d.d_model;
   const float inv_tau = 1.f / p->d.temperature, *over = dloss ? nullptr : R.total + 1;
-  auto scaled = [&](GemmArgs& g) { if (bf16) { g.over = over; g.alpha = inv_tau; } };      // the mean's gradient, see head_epilogue.cuh
-  HEAD_STEP(launch_head_gather(p->d.dtype, R, X, Xc, D, status, st));
   for (int col0 = 0; col0 < p->cols; col0 += p->piece) {
     const int cols = p->cols - col0 < p->piece ? p->cols - col0 : p->piece;
     {
-      GemmArgs g = logits_product(p, R, Xc, W, col0, cols);
+      GemmArgs g = logits_product(p, R, W, col0, cols);
       g.c = dz;
-      if (bf16) {
-        g.epi = 7;
-        g.head = epilogue_of(p, R, col0);
-        g.head.dloss = dloss;
-        g.seq = p->d.seq; g.t_pad = p->base->t_pad;
-      }
+      g.reset_status = col0 == 0;
+      g.epi = 7;
+      g.head = epilogue_of(p, R, col0);
+      g.head.dloss = dloss;
+      if (!bf16) g.head.over = over;
       HEAD_RUN(run_products(p, &g, 1, status, st));
-      if (!bf16)
-        HEAD_STEP(launch_head_grad_f32((float*)dz, R, dloss, p->d.vocab, col0, cols, p->scale, inv_tau, p->d.seq, p->base->t_pad, st));
     }
     GemmArgs gs[2];
     int count = 0;
-    if (dW) {        // a token-axis reduction: dz^T X [vocab, d_model], or X^T dz
+    if (dW) {
       GemmArgs& g = gs[count++];
-      g = GemmArgs{};
-      g.rows = R.n + 1; g.dyn = 2;
-      g.n_terms = 1;
-      if (p->d.vocab_rows) {
-        g.m = cols; g.n = D;
-        g.t[0] = {dz, p->n_pad, 1, Xc, p->n_pad, 0, n, 0};
-        g.c_rows = piece_rows(p, col0, cols);
-      } else {
-        g.m = D; g.n = cols;
-        g.t[0] = {Xc, p->n_pad, 1, dz, p->n_pad, 0, n, 0};
-      }
-      scaled(g);
+      g = dw_product(p, cols);
+      g.rows = R.n + 1;
+      g.t[0].a = p->d.vocab_rows ? dz : R.x;
+      g.t[0].b = p->d.vocab_rows ? R.x : dz;
+      g.c_rows = piece_rows(p, col0, cols);
       g.c = (void*)weights_at(p, dW, col0);
-      g.c_rpad = p->w_rows;
+      if (bf16) { g.over = over; g.alpha = inv_tau; }          // the mean's gradient, see head_epilogue.cuh
     }
-    if (dX) {        // dz W^T, over this piece's columns
+    if (dX) {
       GemmArgs& g = gs[count++];
-      g = GemmArgs{};
-      g.m = n; g.n = D; g.n_terms = 1;
-      g.t[0] = {dz, p->n_pad, 0, weights_at(p, W, col0), p->w_rows, p->d.vocab_rows ? 0 : 1, cols, piece_rows(p, col0, cols)};
-      g.rows = R.n + 1; g.dyn = 1;
-      g.c_rpad = p->n_pad;
-      g.c = acc;
-      if (bf16) { g.ksplit = p->slices; g.acc = acc; g.acc_mode = col0 == 0 ? 1 : 2; }
-      else if (col0 > 0) g.residual = acc;
+      g = dx_product(p, cols);
+      g.rows = R.n + 1;
+      g.t[0].a = dz;
+      g.t[0].b = weights_at(p, W, col0);
+      g.t[0].b_rows = piece_rows(p, col0, cols);
+      g.c = g.acc = acc;
+      g.ksplit = p->slices; g.acc_mode = col0 == 0 ? 1 : 2;
     }
     HEAD_RUN(run_products(p, gs, count, status, st));
   }

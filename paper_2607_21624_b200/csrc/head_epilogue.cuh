@@ -1,15 +1,15 @@
-// The vocabulary's softmax in the epilogue of the head's products: logits leave the accumulator as softmax statistics (forward)
+// The vocabulary's softmax in the epilogue of the head's products, bf16 and fp32: logits leave the accumulator as softmax statistics (forward)
 // or as the gradient of their cross entropy (backward), so that no logit reaches memory.
 //
 // With z the product x.w of a token and a vocabulary column and c = log2 e / temperature,
 //   forward   k = round(c max z),  s = sum of 2^(c z - k)  over a tile's 256 columns, and z itself at the row's targets
 //   backward  dz = (g / s) 2^(c z - k) - g y,  g = the loss's gradient / temperature, y the target probability of the column
-//             (g = 1 for the mean loss, whose 1 / (tokens x temperature) the two products behind are scaled by: with it in dz every
+//             (bf16: g = 1 for the mean loss, whose 1 / (tokens x temperature) the two products behind are scaled by: with it in dz every
 //             token's target would be rounded the same way, and dX and dW come out too large or too small by up to 2^-9)
 // k and s are a whole row's by then (head_combine_kernel).  c z - k is one multiply-add with the same c and k everywhere, so the
 // rounding of k cancels: a target that holds all of its row's probability gives log s = log 1 exactly.  Sums are fp32; dz is
-// rounded to bf16, as an operand of the two products that consume it (half a step of 2^-8 of each value, as large as the
-// rounding of the results).
+// rounded to the storage type, as an operand of the two products that consume it (bf16: half a step of 2^-8 of each value, as
+// large as the rounding of the results).
 //
 // What bounds a tile's epilogue is the exponential unit: 256 columns of 32 rows a warp, a lane's 256 exponentials at 8 clocks a
 // warp instruction are 2048 clocks, beside some 1200 issued instructions; the products of the next tile take 640 clocks per 64 columns
@@ -31,6 +31,7 @@ struct Entries {
   const int32_t* ids;
   long long rows;
   int at, count, next;
+  __device__ __forceinline__ Entries() : ids(nullptr), rows(0), at(0), count(0), next(NONE) {}
   __device__ __forceinline__ Entries(const HeadEpi& H, int row, int count_, int col) : ids(H.ids + row), rows(H.rows), at(0), count(count_) {
     for (int end = count; at < end;) {
       const int mid = (at + end) / 2;
@@ -62,106 +63,124 @@ __device__ __forceinline__ void load_panel(Acc acc, int pn, uint32_t (&v)[64]) {
   acc.wait();
 }
 
+// What a lane knows of its product's row m, and of the columns from `col` on; GRAD: for the backward.
+template <bool GRAD>
+struct Row {
+  Entries e;
+  int row, count;
+  bool live;                  // rows behind the last token's are zero: the reduction over tokens ends inside a k-block
+  float g, gs, k;
+  __device__ __forceinline__ Row() : row(0), count(0), live(false), g(0.f), gs(0.f), k(0.f) {}
+  __device__ __forceinline__ Row(const HeadEpi& H, int m, int col, int seq, int t_pad) : g(0.f), gs(0.f), k(0.f) {
+    live = m < __ldcg(H.n);
+    row = live ? H.row_of[m] : 0;
+    count = live ? H.count[row] : 0;
+    e = Entries(H, row, count, col);
+    if (GRAD && count > 0) {
+      const int b = row / t_pad, t = row - b * t_pad;
+      g = H.dloss ? H.dloss[(long long)b * seq + t] * H.inv_tau : H.over ? H.inv_tau / fmaxf(*H.over, 1.f) : 1.f;
+      k = H.k[row];
+      gs = g / H.sum[row];
+    } else if (GRAD && count < 0) {
+      gs = __int_as_float(0x7fffffff);
+    }
+  }
+};
+
+// 64 columns of logits, those from `col` of the vocabulary on, join the row's (k, s); products at its targets are noted.
+__device__ __forceinline__ void stats64(const HeadEpi& H, Row<false>& R, uint32_t (&v)[64], int col, float& k, float& s) {
+  if (col + 64 > H.vocab) {                               // columns that only pad the weights to whole tiles
+#pragma unroll
+    for (int j = 0; j < 64; ++j) v[j] = col + j < H.vocab ? v[j] : 0xff800000u;
+  }
+  while (__any_sync(0xffffffffu, R.e.next < col + 64)) {
+    if (R.e.next < col + 64) {
+      H.z_at[R.e.at * H.rows + R.row] = __uint_as_float(pick(v, R.e.next - col));
+      R.e.advance();
+    }
+  }
+  float top[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) top[i] = fmaxf(__uint_as_float(v[i]), __uint_as_float(v[4 + i]));
+#pragma unroll
+  for (int j = 8; j < 64; j += 8)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top[i] = tc::fmax3(top[i], __uint_as_float(v[j + i]), __uint_as_float(v[j + 4 + i]));
+  const float was = k;
+  k = fmaxf(k, tc::fmax3(top[0], top[1], fmaxf(top[2], top[3])) * H.scale);
+  const float2 mk = make_float2(-k, -k), c2 = make_float2(H.scale, H.scale);
+  float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+  for (int j = 0; j < 64; j += 2) {
+    const float2 x = __ffma2_rn(make_float2(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), c2, mk);
+    sum[j / 2 % 2] = __fadd2_rn(sum[j / 2 % 2], make_float2(tc::fast_exp2(x.x), tc::fast_exp2(x.y)));
+  }
+  sum[0] = __fadd2_rn(sum[0], sum[1]);
+  s = s * tc::fast_exp2(was - k) + (sum[0].x + sum[0].y);
+}
+
+// 64 columns of logits become their gradient.
+__device__ __forceinline__ void grad64(const HeadEpi& H, Row<true>& R, uint32_t (&v)[64], int col) {
+  const float2 c2 = make_float2(H.scale, H.scale), mk = make_float2(-R.k, -R.k), gs2 = make_float2(R.gs, R.gs);
+#pragma unroll
+  for (int j = 0; j < 64; j += 2) {
+    const float2 x = __ffma2_rn(make_float2(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), c2, mk);
+    const float2 d = __fmul2_rn(make_float2(tc::fast_exp2(x.x), tc::fast_exp2(x.y)), gs2);
+    v[j] = __float_as_uint(d.x);
+    v[j + 1] = __float_as_uint(d.y);
+  }
+  while (__any_sync(0xffffffffu, R.e.next < col + 64)) {
+    const bool mine = R.e.next < col + 64;
+    const int j0 = mine ? R.e.next - col : -1;
+    const float gy = mine ? R.g * H.y[R.e.at * H.rows + R.row] : 0.f;
+#pragma unroll
+    for (int j = 0; j < 64; ++j)
+      if (j == j0) v[j] = __float_as_uint(__uint_as_float(v[j]) - gy);
+    if (mine) R.e.advance();
+  }
+  if (col + 64 > H.vocab) {
+#pragma unroll
+    for (int j = 0; j < 64; ++j) v[j] = col + j < H.vocab ? v[j] : 0u;
+  }
+}
+
 }  // namespace headepi
 
 template <int BN, typename Problem, typename Acc, typename Wait>
 __device__ __forceinline__ bool head_stats_tile(const Problem& P, int m0, int n0, int q, Acc acc, Wait wait) {
   const HeadEpi& H = P.head;
   const int m = m0 + q * 32 + threadIdx.x % 32;
-  const bool live = m < __ldcg(H.n);
-  const int row = live ? H.row_of[m] : 0;
-  headepi::Entries e(H, row, live ? H.count[row] : 0, n0);
+  headepi::Row<false> R(H, m, n0, P.seq, P.t_pad);
   if (!wait()) return false;
   tc::tc_fence_after();
   float k = -INFINITY, s = 0.f;
-  const float2 c2 = make_float2(H.scale, H.scale);
 #pragma unroll 1
-  for (int pn = 0; pn < BN / 64; ++pn) {
-    const int n = n0 + pn * 64;
-    if (n >= H.vocab) break;
+  for (int pn = 0; pn < BN / 64 && n0 + pn * 64 < H.vocab; ++pn) {
     uint32_t v[64];
     headepi::load_panel(acc, pn, v);
-    if (n + 64 > H.vocab) {                               // columns that only pad the weights to whole tiles
-#pragma unroll
-      for (int j = 0; j < 64; ++j) v[j] = n + j < H.vocab ? v[j] : 0xff800000u;
-    }
-    while (__any_sync(0xffffffffu, e.next < n + 64)) {
-      if (e.next < n + 64) {
-        H.z_at[e.at * H.rows + row] = __uint_as_float(headepi::pick(v, e.next - n));
-        e.advance();
-      }
-    }
-    float top[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) top[i] = fmaxf(__uint_as_float(v[i]), __uint_as_float(v[4 + i]));
-#pragma unroll
-    for (int j = 8; j < 64; j += 8)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) top[i] = tc::fmax3(top[i], __uint_as_float(v[j + i]), __uint_as_float(v[j + 4 + i]));
-    const float was = k;
-    k = fmaxf(k, tc::fmax3(top[0], top[1], fmaxf(top[2], top[3])) * H.scale);
-    const float2 mk = make_float2(-k, -k);
-    float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-#pragma unroll
-    for (int j = 0; j < 64; j += 2) {
-      const float2 x = __ffma2_rn(make_float2(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), c2, mk);
-      sum[j / 2 % 2] = __fadd2_rn(sum[j / 2 % 2], make_float2(tc::fast_exp2(x.x), tc::fast_exp2(x.y)));
-    }
-    sum[0] = __fadd2_rn(sum[0], sum[1]);
-    s = s * tc::fast_exp2(was - k) + (sum[0].x + sum[0].y);
+    headepi::stats64(H, R, v, n0 + pn * 64, k, s);
   }
-  if (live) H.part[(long long)(n0 / HEAD_TILE) * H.rows + m] = make_float2(k, s);
+  if (R.live) H.part[(long long)m * H.tiles + n0 / HEAD_TILE] = make_float2(k, s);
   return true;
 }
 
 template <int BN, typename Problem, typename Acc, typename Wait>
 __device__ __forceinline__ bool head_grad_tile(const Problem& P, int m0, int n0, int q, Acc acc, uint32_t stg0, int& pc, Wait wait) {
   const HeadEpi& H = P.head;
-  const int lane = threadIdx.x % 32, m = m0 + q * 32 + lane;
-  const bool live = m < __ldcg(H.n);                    // rows behind the last token's are zero: the reduction over tokens ends inside a k-block
-  const int row = live ? H.row_of[m] : 0, count = live ? H.count[row] : 0;
-  headepi::Entries e(H, row, count, H.col0 + n0);
-  float g = 0.f, gs = 0.f, k = 0.f;
-  if (count > 0) {
-    const int b = row / P.t_pad, t = row - b * P.t_pad;
-    g = H.dloss ? H.dloss[(long long)b * P.seq + t] * H.inv_tau : 1.f;
-    k = H.k[row];
-    gs = g / H.sum[row];
-  } else if (count < 0) {
-    gs = __int_as_float(0x7fffffff);
-  }
+  const int lane = threadIdx.x % 32;
+  headepi::Row<true> R(H, m0 + q * 32 + lane, H.col0 + n0, P.seq, P.t_pad);
   if (!wait()) return false;
   tc::tc_fence_after();
-  const float2 c2 = make_float2(H.scale, H.scale), mk = make_float2(-k, -k), gs2 = make_float2(gs, gs);
 #pragma unroll 1
   for (int pn = 0; pn < BN / 64; ++pn) {
-    const int n = n0 + pn * 64, col = H.col0 + n;
+    const int n = n0 + pn * 64;
     if (n >= P.n) break;
     uint32_t v[64];
     headepi::load_panel(acc, pn, v);
-#pragma unroll
-    for (int j = 0; j < 64; j += 2) {
-      const float2 x = __ffma2_rn(make_float2(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), c2, mk);
-      const float2 d = __fmul2_rn(make_float2(tc::fast_exp2(x.x), tc::fast_exp2(x.y)), gs2);
-      v[j] = __float_as_uint(d.x);
-      v[j + 1] = __float_as_uint(d.y);
-    }
-    while (__any_sync(0xffffffffu, e.next < col + 64)) {
-      const bool mine = e.next < col + 64;
-      const int j0 = mine ? e.next - col : -1;
-      const float gy = mine ? g * H.y[e.at * H.rows + row] : 0.f;
-#pragma unroll
-      for (int j = 0; j < 64; ++j)
-        if (j == j0) v[j] = __float_as_uint(__uint_as_float(v[j]) - gy);
-      if (mine) e.advance();
-    }
-    if (col + 64 > H.vocab) {
-#pragma unroll
-      for (int j = 0; j < 64; ++j) v[j] = col + j < H.vocab ? v[j] : 0u;
-    }
+    headepi::grad64(H, R, v, H.col0 + n);
     uint32_t ow[32];
 #pragma unroll
-    for (int j = 0; j < 32; ++j) ow[j] = count ? tc::pack_bf16(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])) : 0u;
+    for (int j = 0; j < 32; ++j) ow[j] = R.count ? tc::pack_bf16(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])) : 0u;
     // as in epilogue_tile: the staging tile's store two panels ago has been read
     const uint32_t stg = stg0 + (uint32_t)(q * 2 + (pc & 1)) * 4096u;
     __syncwarp();

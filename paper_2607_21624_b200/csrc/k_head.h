@@ -15,21 +15,16 @@ struct HeadRows {
   float *y, *constant;        // constant: sum of y log y
   float *k, *sum;             // softmax statistics
   float* total;               // [2] loss, counted tokens
+  void* x;                    // the products' rows of X, zeros behind them to whole tiles
 };
 
-// Labels, or what teacher_entries has left in `count`, to positions; rows of X with a loss to Xc, zeros behind them to whole tiles.
-cudaError_t launch_head_rows(int dtype, const int32_t* targets, const HeadRows& R, int seq, int t_pad, int vocab, const void* X, void* Xc, int d_model,
+// Labels, or what teacher_entries has left in `count`, to positions; the rows of X with a loss to R.x.
+cudaError_t launch_head_rows(int dtype, const int32_t* targets, const HeadRows& R, int seq, int t_pad, int vocab, const void* X, int d_model,
                              int32_t* status, cudaStream_t st);
 cudaError_t launch_teacher_entries(const int32_t* ids, const float* logits, int top_k, float temperature, const HeadRows& R, int seq, int t_pad,
                                    int vocab, int32_t* status, cudaStream_t st);
-// The rows of X with a loss again (their positions are known); starts a pass.
-cudaError_t launch_head_gather(int dtype, const HeadRows& R, const void* X, void* Xc, int d_model, int32_t* status, cudaStream_t st);
 cudaError_t launch_head_combine(const float2* part, int tiles, const float* z_at, const HeadRows& R, float scale, float* loss, float* total,
                                 float* block_sums, int seq, int t_pad, int32_t* status, cudaStream_t st);
-cudaError_t launch_head_stats_f32(const float* z, const HeadRows& R, int vocab, int col0, int cols, float scale, float2* part, float* z_at,
-                                  cudaStream_t st);
-cudaError_t launch_head_grad_f32(float* z, const HeadRows& R, const float* dloss, int vocab, int col0, int cols, float scale, float inv_tau, int seq,
-                                 int t_pad, cudaStream_t st);
 // dX from the areas' sums, times alpha / max(*over, 1) where `over` is not null
 cudaError_t launch_head_scatter(int dtype, int sm_count, const float* acc, int areas, const HeadRows& R, int d_model, const float* over, float alpha,
                                 void* dX, cudaStream_t st);

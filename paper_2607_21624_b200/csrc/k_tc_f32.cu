@@ -25,6 +25,7 @@
 // 6.5 -> 5.5.  Error against 64 bits relative to the result's norm: 0.4e-7 to 1.8e-7 at 32 to 4096 columns, multiply-adds one after
 // another 1.0e-7 to 9.9e-7; whole steps' outputs: 0.3 to 1.0 of theirs.
 #include "f32_gemm.cuh"
+#include "head_epilogue.cuh"
 #include "launch_memo.h"
 #include "pdl.cuh"
 
@@ -126,7 +127,9 @@ __device__ __noinline__ void plain_tile(const Problem& P, uint32_t tile, uint32_
   __syncthreads();
 }
 
-template <int BN>
+// EPI: what a tile's sums become.  The head's epilogues take whole sums: one slice.
+enum { F32_PLAIN = 0, F32_HEAD_STATS, F32_HEAD_GRAD };
+template <int BN, int EPI>
 __global__ void __launch_bounds__(THREADS, 1) gemm_tc_f32_kernel(const __grid_constant__ Group G) {
   using SM = Smem<BN>;
   constexpr int STAGES = SM::STAGES;
@@ -140,11 +143,13 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_tc_f32_kernel(const __grid_co
   auto added = [&](int b) { return bars + 8u * (2 * STAGES + 4 + b); };     // the accumulator has been read
   const int warp = (int)tc::uniform(threadIdx.x / 32), lane = threadIdx.x % 32;
   const tc::Status status(G.status, G.reset_status);
-  // work unit: (problem, tile, slice); the slices of a tile are the blocks of a cluster
+  // work unit: (problem, tile, area, slice); the slices of a tile are the blocks of a cluster
   const int slice = blockIdx.x % G.slices;
   int w = blockIdx.x / G.slices, pi = 0;
-  while (w >= G.p[pi].tiles_m * G.p[pi].tiles_n) { w -= G.p[pi].tiles_m * G.p[pi].tiles_n; ++pi; }
+  while (w >= G.p[pi].tiles_m * G.p[pi].tiles_n * G.p[pi].areas) { w -= G.p[pi].tiles_m * G.p[pi].tiles_n * G.p[pi].areas; ++pi; }
   const Problem& P = G.p[pi];
+  const int area = w % P.areas;
+  w /= P.areas;
   const int m0 = (w % P.tiles_m) * BM, n0 = (w / P.tiles_m) * BN;
   int total_kb = P.total_kb;
   if (P.dyn) {                               // fewer rows, or less to reduce, than the launch was made for
@@ -177,8 +182,13 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_tc_f32_kernel(const __grid_co
   asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem_base) : "r"(slot));
   tmem_base = tc::uniform(tmem_base);
   pdl_launch_dependents();
-  const int kb_begin = gemm_slice_begin(total_kb, G.slices, slice), n_kb = gemm_slice_begin(total_kb, G.slices, slice + 1) - kb_begin;
+  const int area_kb = gemm_slice_begin(total_kb, P.areas, area), area_n = gemm_slice_begin(total_kb, P.areas, area + 1) - area_kb;
+  const int kb_begin = area_kb + gemm_slice_begin(area_n, G.slices, slice), n_kb = area_kb + gemm_slice_begin(area_n, G.slices, slice + 1) - kb_begin;
 
+  // the head: a lane of the last eight warps has half a row of the tile, 64 columns
+  static_assert(EPI == F32_PLAIN || BN == 128, "half a row is 64 columns");
+  headepi::Row<EPI == F32_HEAD_GRAD> R;
+  const int half_m = m0 + warp % 4 * 32 + lane, half_n = n0 + (warp - 10) / 4 * 64;
   if (warp == 0) {
     if (lane == 0) {
       auto load_b = [&](int it, int t, int k) {
@@ -304,6 +314,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_tc_f32_kernel(const __grid_co
     for (int i = 0; i < N / 2; ++i) sum[i] = make_float2(0.f, 0.f);
     pdl_wait();
     f32g::group_chores(G, threadIdx.x - 10 * 32, 256);
+    if constexpr (EPI != F32_PLAIN) R = headepi::Row<EPI == F32_HEAD_GRAD>(P.head, half_m, P.head.col0 + half_n, P.seq, P.t_pad);
     for (int it = 0; it < n_kb; ++it) {
       const int b = it & 1;
       if (!tc::mbar_wait(done(b), (it >> 1) & 1, status, 138)) break;
@@ -340,11 +351,32 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_tc_f32_kernel(const __grid_co
   if (again) plain_tile<BN>(P, base, base + SM::PARTS_OFF, m0, n0, kb_begin, kb_begin + n_kb);
   if (G.slices > 1) tc::cluster_sync_all();
   if (warp == 1) tc::tmem_dealloc(tmem_base, TMEM_COLS);
-  f32g::finish_tile<BM, BN, SM::LD, THREADS>(P, G.slices, slice, base, m0, n0);
+  if constexpr (EPI != F32_PLAIN) {
+    if (warp >= 10 && half_n < P.n) {
+      const uint32_t at = base + (uint32_t)((warp % 4 * 32 + lane) * SM::LD + (half_n - n0)) * 4;
+      uint32_t v[64];
+#pragma unroll
+      for (int j = 0; j < 64; j += 4) *reinterpret_cast<float4*>(&v[j]) = lds4(at + j * 4);
+      if constexpr (EPI == F32_HEAD_STATS) {
+        float k = -INFINITY, s = 0.f;
+        headepi::stats64(P.head, R, v, half_n, k, s);
+        if (R.live) P.head.part[(long long)half_m * P.head.tiles + half_n / HEAD_TILE_F32] = make_float2(k, s);
+      } else {
+        headepi::grad64(P.head, R, v, P.head.col0 + half_n);
+#pragma unroll
+        for (int j = 0; j < 64; ++j) v[j] = R.count ? v[j] : 0u;
+#pragma unroll
+        for (int j = 0; j < 64; j += 4) sts4(at + j * 4, &v[j]);
+      }
+    }
+    if (EPI == F32_HEAD_STATS) return;
+    __syncthreads();
+  }
+  f32g::finish_tile<BM, BN, SM::LD, THREADS>(P, G.slices, slice, base, m0, n0, area * P.area_stride);
   if (G.slices > 1) tc::cluster_sync_all();      // no block leaves while another may still read its partial tile
 }
 
-struct Launch { Group G; int grid, bn; };
+struct Launch { Group G; int grid, bn; void (*kernel)(const Group); };
 
 // Tile width (128, 64) and slices (1, 2, 4, 8: blocks of a cluster) of a launch: the shortest list schedule, in the order of the
 // grid, of its tiles over the clusters that fit the part at once.  Measured: a block takes some 6 us (64 columns: 4.5) to come up,
@@ -352,12 +384,13 @@ struct Launch { Group G; int grid, bn; };
 // slices of 128 and 64 columns (us): three problems of 768 columns 22.6 30 47, 36 48 73; one of them 21.7 15.2 22.6, 18 24 27; dWo with
 // dA 23.7 28.6 36, 35 37 48; dWq, dWk, dWv with dXn 74 61 76, 80 89 117.  128 x 512 x 512: 16.0 12.2 9.7, 13.2 10.2 7.9.
 struct Choice { int bn, slices; };
-Choice choose(const fbl_plan* p, const GemmArgs* gs, const int* order, int count) {
+Choice choose(const fbl_plan* p, const GemmArgs* gs, const int* order, int count, double* time = nullptr) {
   Choice best = {128, 1};
   double best_t = 1e30;
   for (int bn = 128; bn >= 64; bn -= 64)
     for (int s = 1; s <= 8; s *= 2) {
-      if ((p->knob_f32_bn && bn != p->knob_f32_bn) || (p->knob_f32_slices && s != p->knob_f32_slices)) continue;
+      if (gs[0].epi >= 6 && (bn != 128 || s != 1)) continue;
+      if ((p->knob_f32_bn && bn != p->knob_f32_bn && gs[0].epi < 6) || (p->knob_f32_slices && s != p->knob_f32_slices && gs[0].epi < 6)) continue;
       constexpr int MAX_SLOTS = 256;
       double end[MAX_SLOTS], cost[f32g::MAX_PROBLEMS], load = 0, whole = 0;      // end: a heap, the earliest on top
       // clusters of 4 and 8 do not fill every group of SMs that shares a scheduler
@@ -368,8 +401,10 @@ Choice choose(const fbl_plan* p, const GemmArgs* gs, const int* order, int count
         const GemmArgs& g = gs[order[j]];
         int kb = 0;
         for (int i = 0; i < g.n_terms; ++i) kb += (g.t[i].k + BK - 1) / BK;
+        const int areas = g.acc_mode && g.ksplit > 1 ? g.ksplit : 1;
+        kb = (kb + areas - 1) / areas;
         cost[j] = (bn == 128 ? 6.0 : 4.5) + (bn == 128 ? 1.06 : 0.9) * ((kb + s - 1) / s) + (s > 1 ? 0.3 : 0.0);
-        units[j] = (long long)((g.m + BM - 1) / BM) * ((g.n + bn - 1) / bn);
+        units[j] = (long long)((g.m + BM - 1) / BM) * ((g.n + bn - 1) / bn) * areas;
         load += units[j] * cost[j] / slots;
         const long long rounds = units[j] / slots > 1 ? units[j] / slots - 1 : 0;     // rounds that leave the order as it is
         whole += rounds * cost[j];
@@ -393,6 +428,7 @@ Choice choose(const fbl_plan* p, const GemmArgs* gs, const int* order, int count
       t += whole;
       if (t < best_t * 0.99) { best_t = t; best = {bn, s}; }
     }
+  if (time) *time = best_t;
   return best;
 }
 
@@ -400,6 +436,7 @@ Choice choose(const fbl_plan* p, const GemmArgs* gs, const int* order, int count
 
 cudaError_t launch_gemm_tc_f32_group(const fbl_plan* p, const GemmArgs* gs, int count, int32_t* status, cudaStream_t st) {
   if (count < 1 || count > f32g::MAX_PROBLEMS) return cudaErrorInvalidValue;
+  if (gs[0].epi >= 6 && (count != 1 || !gs[0].head.n || gs[0].acc_mode || gs[0].residual || gs[0].bias)) return cudaErrorInvalidValue;
   LaunchKey key;
   gemm_group_key(key, gs, count);
   return LaunchMemo<Launch, 12>::run(p, FBL_MEMO_TC_F32_GEMM, key,
@@ -409,18 +446,35 @@ cudaError_t launch_gemm_tc_f32_group(const fbl_plan* p, const GemmArgs* gs, int 
         const Choice c = choose(p, gs, order, count);
         if (!f32g::fill_group(L.G, gs, count, order, BM, c.bn, BK)) return cudaErrorInvalidValue;
         L.grid = 0;
-        for (int i = 0; i < count; ++i) L.grid += L.G.p[i].tiles_m * L.G.p[i].tiles_n * c.slices;
+        for (int i = 0; i < count; ++i) L.grid += L.G.p[i].tiles_m * L.G.p[i].tiles_n * L.G.p[i].areas * c.slices;
         L.G.slices = c.slices;
         L.bn = c.bn;
-        const cudaError_t e = cudaFuncSetAttribute(gemm_tc_f32_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Smem<128>::TOTAL);
-        return e != cudaSuccess ? e : cudaFuncSetAttribute(gemm_tc_f32_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Smem<64>::TOTAL);
+        L.kernel = gs[0].epi == 6 ? gemm_tc_f32_kernel<128, F32_HEAD_STATS> : gs[0].epi == 7 ? gemm_tc_f32_kernel<128, F32_HEAD_GRAD>
+                   : c.bn == 128 ? gemm_tc_f32_kernel<128, F32_PLAIN> : gemm_tc_f32_kernel<64, F32_PLAIN>;
+        return cudaFuncSetAttribute(L.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(c.bn == 128 ? Smem<128>::TOTAL : Smem<64>::TOTAL));
       },
       [&](Launch& L) { return f32g::point_group(L.G, gs, status); },
       [&](const Launch& L) {
-        auto go = [&](auto kernel, size_t smem) {
-          if (L.G.slices > 1) return launch_cluster(kernel, dim3(L.grid), dim3(THREADS), smem, st, L.G.slices, true, L.G);
-          return launch_pdl(kernel, dim3(L.grid), dim3(THREADS), smem, st, L.G);
-        };
-        return L.bn == 128 ? go(gemm_tc_f32_kernel<128>, Smem<128>::TOTAL) : go(gemm_tc_f32_kernel<64>, Smem<64>::TOTAL);
+        const size_t smem = L.bn == 128 ? Smem<128>::TOTAL : Smem<64>::TOTAL;
+        if (L.G.slices > 1) return launch_cluster(L.kernel, dim3(L.grid), dim3(THREADS), smem, st, L.G.slices, true, L.G);
+        return launch_pdl(L.kernel, dim3(L.grid), dim3(THREADS), smem, st, L.G);
       });
+}
+
+int gemm_tc_f32_choose_areas(const fbl_plan* p, GemmArgs* gs, int count) {
+  static const int cand[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32};
+  GemmArgs& g = gs[count - 1];
+  int best = 1;
+  double best_t = 1e300;
+  for (int areas : cand) {
+    if (areas > 1 && (g.t[0].k + BK - 1) / BK < 4 * areas) break;
+    g.acc_mode = 1; g.ksplit = areas;
+    int order[f32g::MAX_PROBLEMS];
+    f32g::longest_first(gs, count, order);
+    double t;
+    choose(p, gs, order, count, &t);
+    t += areas * (double)g.m * g.n * 8 / 6.5e6;                    // microseconds: written once, read once
+    if (t < 0.98 * best_t) { best = areas; best_t = t; }
+  }
+  return best;
 }

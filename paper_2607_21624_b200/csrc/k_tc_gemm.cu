@@ -65,6 +65,9 @@ struct alignas(64) TcGroup {
   int32_t* status;
   const int32_t* rows;                       // see GemmArgs
   int dynamic;                               // 1: the work list depends on it
+  // Of two problems, the first with longer units than the second: deal them out as Deal does, with a unit's clocks per k-block, and
+  // at least `floor` (its epilogue) beside them (0: in turn)
+  float kb_clocks, unit_clocks, floor_clocks;
   // Optional chores for the epilogue warps while the first tile's main loop runs: zero-fill a buffer that a later
   // kernel of the pass adds into (16-byte units, dealt evenly to the blocks), and reset the pass's status word.
   uint4* zero_ptr;
@@ -113,27 +116,87 @@ __device__ __forceinline__ int dynamic_rows(const TcGroup& G) {
   return __ldcg(G.rows);
 }
 
+__device__ __forceinline__ void coord(const TcProblem& P, int rows, int p, int slice, int m0, int n0, TileCoord* tc_out) {
+  const int kb = kblocks_of(P, rows), per = (kb + P.ksplit - 1) / P.ksplit;
+  tc_out->prob = p;
+  tc_out->m0 = m0;
+  tc_out->n0 = n0;
+  tc_out->slice = slice;
+  tc_out->kb0 = slice * per;
+  tc_out->kb1 = min(kb, (slice + 1) * per);
+}
+// Tiles of a problem: 128 x BN, or a pair's 256 x 256.  Tall problems go in bands of eight row
+// tiles of pairs: the 74 tiles at work then share eight row tiles and nine column tiles of operands instead of 32 and two or three, which
+// L2 holds (8192 x 4096 attention step: 5060 -> 4945 us, its four product launches 535, 172, 378, 1191 -> 505, 167, 364, 1131; bands
+// of 16 the same).  Up to 16 row tiles fit as they are (4096 x 2048 x 8192 feed-forward in bands of eight: 88 -> 92 us a launch).
+constexpr int PAIR_BAND = 8, PAIR_BAND_FROM = 16;
 template <int BN>
-__device__ __forceinline__ bool tile_at(const TcGroup& G, int rows, int w, TileCoord* tc_out) {
-  for (int p = 0; p < G.count; ++p) {
-    const TcProblem& P = G.p[p];
-    const int tm = (rows_of(P, rows) + BM - 1) / BM, tn = (P.n + BN - 1) / BN;
-    const int units = tm * tn * P.ksplit;
-    if (w < units) {
-      const int slice = w % P.ksplit, t = w / P.ksplit;        // slices of one tile are neighbours in the list
-      tc_out->prob = p;
-      tc_out->m0 = (t % tm) * BM;
-      tc_out->n0 = (t / tm) * BN;
-      const int kb = kblocks_of(P, rows), per = (kb + P.ksplit - 1) / P.ksplit;
-      tc_out->slice = slice;
-      tc_out->kb0 = slice * per;
-      tc_out->kb1 = min(kb, (slice + 1) * per);
+struct OneBlock {
+  static __device__ __forceinline__ int tm(const TcProblem& P, int rows) { return (rows_of(P, rows) + BM - 1) / BM; }
+  static __device__ __forceinline__ int units(const TcProblem& P, int rows) { return tm(P, rows) * ((P.n + BN - 1) / BN) * P.ksplit; }
+  static __device__ __forceinline__ void at(const TcProblem& P, int rows, int p, int w, TileCoord* tc_out) {
+    const int m = tm(P, rows), slice = w % P.ksplit, t = w / P.ksplit;        // slices of one tile are neighbours in the list
+    coord(P, rows, p, slice, (t % m) * BM, (t / m) * BN, tc_out);
+  }
+};
+struct BlockPair {
+  static __device__ __forceinline__ int tm(const TcProblem& P, int rows) { return (rows_of(P, rows) + 255) / 256; }
+  static __device__ __forceinline__ int units(const TcProblem& P, int rows) { return tm(P, rows) * ((P.n + 255) / 256) * P.ksplit; }
+  static __device__ __forceinline__ void at(const TcProblem& P, int rows, int p, int w, TileCoord* tc_out) {
+    const int m = tm(P, rows), tn = (P.n + 255) / 256, slice = w % P.ksplit, t = w / P.ksplit;
+    const int band = m > PAIR_BAND_FROM ? PAIR_BAND : m, at = t / (band * tn), h = min(band, m - at * band), u = t - at * band * tn;
+    coord(P, rows, p, slice, (at * band + u % h) * 256, (u / h) * 256, tc_out);
+  }
+};
+
+// What a block (a pair) works through.  Units are dealt out in turn, problem by problem.  Of two problems, whose units differ in length
+// and may be known to the device alone, that leaves the blocks with a unit more of the long ones behind; there the other blocks
+// first get as many short ones as a long one is worth, and the rest goes round.  Every other block takes its short ones first, so
+// that a problem bound by what it reads and one bound by what it writes share the time.
+template <typename Tiles>
+struct Deal {
+  int slot, slots, rows;
+  int longs, shorts, light, head, base;      // this block's units; blocks that go first; short units that they get first, and all of those
+  bool balanced;
+  __device__ __forceinline__ Deal(const TcGroup& G, int slot_, int slots_, int rows_) : slot(slot_), slots(slots_), rows(rows_), balanced(G.kb_clocks > 0.f) {
+    if (!balanced) return;
+    const TcProblem &A = G.p[0], &B = G.p[1];
+    const int u = Tiles::units(A, rows), v = Tiles::units(B, rows), over = u % slots;
+    const int kb = kblocks_of(A, rows), per = (kb + A.ksplit - 1) / A.ksplit;
+    const float a = fmaxf(per * G.kb_clocks + G.unit_clocks, G.floor_clocks), b = fmaxf(kblocks_of(B, rows) * G.kb_clocks + G.unit_clocks, G.floor_clocks);
+    light = slots - over;
+    head = over ? min((int)(a / b + 0.5f), v / light) : 0;
+    base = light * head;
+    longs = u / slots + (slot < over);
+    const int rest = v - base - slot;
+    shorts = (slot < over ? 0 : head) + (rest > 0 ? (rest + slots - 1) / slots : 0);
+  }
+  __device__ __forceinline__ bool at(const TcGroup& G, int k, TileCoord* tc_out) const {
+    if (balanced) {
+      if (k >= longs + shorts) return false;
+      const bool odd = slot & 1;
+      if (odd ? k >= shorts : k < longs) {
+        Tiles::at(G.p[0], rows, 0, slot + (odd ? k - shorts : k) * slots, tc_out);
+        return true;
+      }
+      int j = odd ? k : k - longs;
+      const int over = slots - light;
+      if (slot >= over) {
+        if (j < head) { Tiles::at(G.p[1], rows, 1, slot - over + j * light, tc_out); return true; }
+        j -= head;
+      }
+      Tiles::at(G.p[1], rows, 1, base + slot + j * slots, tc_out);
       return true;
     }
-    w -= units;
+    int w = slot + k * slots;
+    for (int p = 0; p < G.count; ++p) {
+      const int units = Tiles::units(G.p[p], rows);
+      if (w < units) { Tiles::at(G.p[p], rows, p, w, tc_out); return true; }
+      w -= units;
+    }
+    return false;
   }
-  return false;
-}
+};
 
 __device__ __forceinline__ float tanh_fast(float x) {
   float y;
@@ -197,6 +260,10 @@ __device__ __forceinline__ bool epilogue_tile(const TcProblem& P, int m0, int n0
       const int c = n0 + lane * (BN / 32) + k;
       bl[k] = c < P.n ? bias[c] : 0.f;
     }
+  }
+  float alpha = 1.f;
+  if constexpr (EPI == EPI_NONE) {
+    if (P.over) alpha = P.alpha / fmaxf(*P.over, 1.f);
   }
   if (!wait()) return false;
   tc::tc_fence_after();
@@ -323,9 +390,8 @@ __device__ __forceinline__ bool epilogue_tile(const TcProblem& P, int m0, int n0
     }
     if constexpr (EPI == EPI_NONE) {
       if (P.over) {
-        const float a = P.alpha / fmaxf(*P.over, 1.f);
 #pragma unroll
-        for (int j = 0; j < 64; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * a);
+        for (int j = 0; j < 64; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * alpha);
       }
     }
     bool bias_left = bias != nullptr;
@@ -483,8 +549,8 @@ __global__ void __maxnreg__(ESETS == 2 ? 168 : EPI == EPI_ACT ? 255 : 224) gemm_
     // Weights do not depend on the kernel before this one: their tiles for the first stages of the first
     // output tile are requested before waiting for that kernel, hiding their (cold) latency.
     int prefilled = 0;
-    const int rows = dynamic_rows(G);
-    if (tile_at<BN>(G, rows, blockIdx.x, &tcd) && G.p[tcd.prob].b_static && G.p[tcd.prob].ksplit == 1) {
+    const Deal<OneBlock<BN>> deal(G, blockIdx.x, gridDim.x, dynamic_rows(G));
+    if (deal.at(G, 0, &tcd) && G.p[tcd.prob].b_static && G.p[tcd.prob].ksplit == 1) {
       const TcProblem& P = G.p[tcd.prob];
       if (leader) { tc::tma_prefetch_desc(&P.ta[0]); tc::tma_prefetch_desc(&P.tb[0]); }
       const int n = P.kblocks[0] < STAGES ? P.kblocks[0] : STAGES;
@@ -499,7 +565,7 @@ __global__ void __maxnreg__(ESETS == 2 ? 168 : EPI == EPI_ACT ? 255 : 224) gemm_
     }
     pdl_wait();
     if (G.late_trigger && leader) late_trigger(G);
-    for (int w = blockIdx.x; ok && tile_at<BN>(G, rows, w, &tcd); w += gridDim.x) {
+    for (int k = 0; ok && deal.at(G, k, &tcd); ++k) {
       const TcProblem& P = G.p[tcd.prob];
       for (int t = 0; t < P.n_terms && ok; ++t) {
         int kb = t == 0 ? tcd.kb0 : 0;
@@ -538,8 +604,8 @@ __global__ void __maxnreg__(ESETS == 2 ? 168 : EPI == EPI_ACT ? 255 : 224) gemm_
     bool ok = true;
     TileCoord tcd;
     const uint32_t hi = tc::smem_desc_hi(1024);
-    const int rows = dynamic_rows(G);
-    for (int w = blockIdx.x; ok && tile_at<BN>(G, rows, w, &tcd); w += gridDim.x, ++ti) {
+    const Deal<OneBlock<BN>> deal(G, blockIdx.x, gridDim.x, dynamic_rows(G));
+    for (; ok && deal.at(G, ti, &tcd); ++ti) {
       const TcProblem& P = G.p[tcd.prob];
       const int ab = ti & 1;
       if (!tc::mbar_wait_warp(acc_empty(ab), ((ti >> 1) & 1) ^ 1, status, 104)) { ok = false; break; }
@@ -574,11 +640,11 @@ __global__ void __maxnreg__(ESETS == 2 ? 168 : EPI == EPI_ACT ? 255 : 224) gemm_
     pdl_wait();                                       // the previous kernel may still be reading what we overwrite
     group_chores(G, threadIdx.x - 64, 128 * ESETS);
     const int q = warp % 4;                           // the TMEM lane quarter this warp may access
-    const int rows = dynamic_rows(G);
+    const Deal<OneBlock<BN>> deal(G, blockIdx.x, gridDim.x, dynamic_rows(G));
     int ti = 0, pc = 0;                               // tiles and panels done by this warp
     bool ok = true;
     TileCoord tcd;
-    for (int w = blockIdx.x; ok && tile_at<BN>(G, rows, w, &tcd); w += gridDim.x, ++ti) {
+    for (; ok && deal.at(G, ti, &tcd); ++ti) {
       const TcProblem& P = G.p[tcd.prob];
       const int ab = ti & 1;
       const bool ready = fused_epilogue_tile<BN, ESETS, EPI>(P, tcd.m0, tcd.n0, tcd.slice, q, TmemAcc{tmem_base + ((uint32_t)(q * 32) << 16) + ab * BN}, base + SP::STG_OFF, pc, [&] {
@@ -612,33 +678,6 @@ struct PairSmem {
   static constexpr uint32_t N_BARS = 2 * PAIR_STAGES + 4;
   static constexpr uint32_t TOTAL = BAR_OFF + 8 * N_BARS + 16 + 1024;
 };
-
-// work list in 256 x 256 tiles (ksplit slices as in tile_at); m0 / n0 are the pair's.  Tall problems go in bands of eight row
-// tiles: the 74 tiles at work then share eight row tiles and nine column tiles of operands instead of 32 and two or three, which
-// L2 holds (8192 x 4096 attention step: 5060 -> 4945 us, its four product launches 535, 172, 378, 1191 -> 505, 167, 364, 1131; bands
-// of 16 the same).  Up to 16 row tiles fit as they are (4096 x 2048 x 8192 feed-forward in bands of eight: 88 -> 92 us a launch).
-constexpr int PAIR_BAND = 8, PAIR_BAND_FROM = 16;
-__device__ __forceinline__ bool pair_tile_at(const TcGroup& G, int rows, int w, TileCoord* tc_out) {
-  for (int p = 0; p < G.count; ++p) {
-    const TcProblem& P = G.p[p];
-    const int tm = (rows_of(P, rows) + 255) / 256, tn = (P.n + 255) / 256;
-    const int units = tm * tn * P.ksplit;
-    if (w < units) {
-      const int slice = w % P.ksplit, t = w / P.ksplit;
-      tc_out->prob = p;
-      const int band = tm > PAIR_BAND_FROM ? PAIR_BAND : tm, at = t / (band * tn), h = min(band, tm - at * band), u = t - at * band * tn;
-      tc_out->m0 = (at * band + u % h) * 256;
-      tc_out->n0 = (u / h) * 256;
-      const int kb = kblocks_of(P, rows), per = (kb + P.ksplit - 1) / P.ksplit;
-      tc_out->slice = slice;
-      tc_out->kb0 = slice * per;
-      tc_out->kb1 = min(kb, (slice + 1) * per);
-      return true;
-    }
-    w -= units;
-  }
-  return false;
-}
 
 template <int EPI>
 __global__ void __cluster_dims__(2, 1, 1) __maxnreg__(EPI == EPI_ACT ? 255 : 224) gemm_tc_pair_kernel(const __grid_constant__ TcGroup G) {
@@ -692,8 +731,8 @@ __global__ void __cluster_dims__(2, 1, 1) __maxnreg__(EPI == EPI_ACT ? 255 : 224
     const uint32_t full0 = tc::map_to_cta(full(0), 0);
     pdl_wait();
     if (G.late_trigger && leader) late_trigger(G);
-    const int rows = dynamic_rows(G);
-    for (int w = pair_id; ok && pair_tile_at(G, rows, w, &tcd); w += n_pairs) {
+    const Deal<BlockPair> deal(G, pair_id, n_pairs, dynamic_rows(G));
+    for (int k = 0; ok && deal.at(G, k, &tcd); ++k) {
       const TcProblem& P = G.p[tcd.prob];
       const int m0 = tcd.m0 + (int)rank * 128, n0 = tcd.n0 + (int)rank * 128;
       for (int t = 0; t < P.n_terms && ok; ++t) {
@@ -724,8 +763,8 @@ __global__ void __cluster_dims__(2, 1, 1) __maxnreg__(EPI == EPI_ACT ? 255 : 224
     bool ok = true;
     TileCoord tcd;
     const uint32_t hi = tc::smem_desc_hi(1024);
-    const int rows = dynamic_rows(G);
-    for (int w = pair_id; ok && pair_tile_at(G, rows, w, &tcd); w += n_pairs, ++ti) {
+    const Deal<BlockPair> deal(G, pair_id, n_pairs, dynamic_rows(G));
+    for (; ok && deal.at(G, ti, &tcd); ++ti) {
       const TcProblem& P = G.p[tcd.prob];
       const int ab = ti & 1;
       if (!tc::mbar_wait_warp(acc_empty(ab), ((ti >> 1) & 1) ^ 1, status, 114)) { ok = false; break; }
@@ -758,11 +797,11 @@ __global__ void __cluster_dims__(2, 1, 1) __maxnreg__(EPI == EPI_ACT ? 255 : 224
     pdl_wait();
     group_chores(G, threadIdx.x - 64, 128);
     const int q = warp % 4;
-    const int rows = dynamic_rows(G);
+    const Deal<BlockPair> deal(G, pair_id, n_pairs, dynamic_rows(G));
     int ti = 0, pc = 0;
     bool ok = true;
     TileCoord tcd;
-    for (int w = pair_id; ok && pair_tile_at(G, rows, w, &tcd); w += n_pairs, ++ti) {
+    for (; ok && deal.at(G, ti, &tcd); ++ti) {
       const TcProblem& P = G.p[tcd.prob];
       const int ab = ti & 1;
       const int m0 = tcd.m0 + (int)rank * 128;
@@ -842,7 +881,7 @@ __global__ void __launch_bounds__(320, 1) gemm_tc_split_kernel(const __grid_cons
 
   const int slice = blockIdx.x % G.slices;
   TileCoord tcd;
-  tile_at<BN>(G, 0, blockIdx.x / G.slices, &tcd);
+  Deal<OneBlock<BN>>(G, blockIdx.x / G.slices, 1 << 20, 0).at(G, 0, &tcd);
   const TcProblem& P = G.p[tcd.prob];
   int total = 0;
   for (int t = 0; t < P.n_terms; ++t) total += P.kblocks[t];
@@ -1336,6 +1375,27 @@ bool slim_legal(const GemmArgs* gs, int count, int sm_count) {
   return legal && tiles <= sm_count;
 }
 
+// Two problems dealt out as Deal does, the first with the longer units.  Blocks whose epilogues take longer than what they add up have
+// two sets of epilogue warps.
+bool two_sets_pay(const TileCost& c, const TileWork& w) { return c.m == 128 && c.n > 64 && (w.kb + w.split - 1) / w.split * c.kb + c.unit < c.epilogue; }
+double deal_makespan(const TileCost& c, const TileWork& a, const TileWork& b, int slots) {
+  auto units = [&](const TileWork& w) { return (double)((w.m + c.m - 1) / c.m) * ((w.n + c.n - 1) / c.n) * w.split; };
+  const double epilogue = two_sets_pay(c, b) ? 0.5 * c.epilogue : c.epilogue;
+  auto length = [&](const TileWork& w) { return std::max((w.kb + w.split - 1) / w.split * c.kb + c.unit, epilogue); };
+  const double u = units(a), v = units(b), la = length(a), lb = length(b);
+  const double whole = (double)((long long)((u + slots - 1) / slots)) * la;
+  return std::max(whole, (u * la + v * lb) / slots + 0.5 * lb) + c.epilogue + c.fixed;
+}
+int best_deal(const TileWork& a, const TileWork& b, int sm_count, bool pairs, double* clocks) {
+  int kind = TILE_NARROW;
+  *clocks = 1e300;
+  for (int k = TILE_NARROW; k <= (pairs ? TILE_PAIR : TILE_WIDE); ++k) {
+    const double t = deal_makespan(TILE_COST[k], a, b, k == TILE_PAIR ? sm_count / 2 : sm_count);
+    if (t < *clocks) { *clocks = t; kind = k; }
+  }
+  return kind;
+}
+
 int best_tile(const TileWork* w, int count, int sm_count, bool pairs, double* clocks) {
   int kind = TILE_NARROW;
   *clocks = 1e300;
@@ -1363,6 +1423,24 @@ static cudaError_t make_group(GroupLaunch& L, const fbl_plan* p, const GemmArgs*
   if (gs[0].epi >= 6) {
     const double one = tile_makespan(TILE_COST[TILE_WIDE], w, count, p->sm_count), two = tile_makespan(TILE_COST[TILE_PAIR], w, count, p->sm_count / 2);
     return make_group_head(L, p, gs, count, pair_mode >= 0 ? pair_mode == 1 : two < one);
+  }
+  if (gs[0].rows && count == 2) {
+    // dX's slices and dW's tiles, or the other way round: the longer ones first
+    const int first = w[1].kb / w[1].split > w[0].kb / w[0].split ? 1 : 0;
+    const TileWork a = w[first], b = w[1 - first];
+    double clocks;
+    kind = best_deal(a, b, p->sm_count, pair_mode != 0, &clocks);
+    if (two_sets_pay(TILE_COST[TILE_WIDE], b)) kind = TILE_WIDE;
+    if (pair_mode == 1) kind = TILE_PAIR;
+    for (int i = 0; i < 2; ++i) { L.order[i] = i ? 1 - first : first; by_length[i] = gs[L.order[i]]; }
+    by_length[0].serial = gs[0].serial; by_length[0].late_trigger = gs[0].late_trigger;
+    const TileCost& c = TILE_COST[kind];
+    const bool two = two_sets_pay(c, b);
+    cudaError_t e = kind == TILE_PAIR ? make_group_pair(L, p, by_length, 2)
+                    : kind == TILE_WIDE ? make_group_bn<256, 4>(L, p, by_length, 2, two ? 2 : 0) : make_group_bn<128, 6>(L, p, by_length, 2, two ? 2 : 0);
+    L.idle = 0;
+    L.G.kb_clocks = (float)c.kb; L.G.unit_clocks = (float)c.unit; L.G.floor_clocks = (float)(two ? 0.5 * c.epilogue : c.epilogue);
+    return e;
   }
   if (pair_mode == 1) {
     kind = TILE_PAIR;
@@ -1455,20 +1533,30 @@ int gemm_tc_choose_split(int sm_count, const GemmShape* sh, int count, bool zero
   return best;
 }
 
-int gemm_tc_choose_own_slices(int sm_count, const GemmShape* sh, int count) {
+int gemm_tc_choose_own_slices(int sm_count, const GemmShape* dw, const GemmShape& dx) {
+  // Few tokens: dW is bound by what it writes, dX by what it reads, and the two share the time if a third of the blocks take dX first
+  // while the others write (50 tokens of 768 over 50257 columns, 3 dX tiles: 48 units 35 us, 24 and 36 units 51 and 57, 72 to 144
+  // units 41 to 43).
+  if (dw && two_sets_pay(TILE_COST[TILE_WIDE], {dw->m, dw->n, dw->kblocks, 1})) {
+    const long long tiles = (dx.m + 127) / 128 * ((dx.n + 255) / 256);
+    return (int)std::max(1ll, std::min(sm_count / 3 / tiles, (long long)dx.kblocks / 8));
+  }
   static const int cand[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
   double best_cost = 1e300;
   int best = 1;
   for (int S : cand) {
-    if (S > 1 && sh[count - 1].kblocks / S < 8) break;
-    TileWork w[MAX_PROBLEMS];
-    for (int i = 0; i < count; ++i) w[i] = {sh[i].m, sh[i].n, sh[i].kblocks, i == count - 1 ? S : 1};
+    if (S > 1 && dx.kblocks / S < 8) break;
+    const TileWork x = {dx.m, dx.n, dx.kblocks, S};
     double cost;
-    best_tile(w, count, sm_count, true, &cost);
-    // the areas are written once and read once, at some 3400 bytes a clock
-    cost += (double)S * sh[count - 1].m * sh[count - 1].n * 8 / 3400;
+    if (dw) {
+      const TileWork v = {dw->m, dw->n, dw->kblocks, 1};
+      if (x.kb / S > v.kb) best_deal(x, v, sm_count, true, &cost);
+      else best_deal(v, x, sm_count, true, &cost);
+    } else {
+      best_tile(&x, 1, sm_count, true, &cost);
+    }
+    cost += (double)S * dx.m * dx.n * 8 / 3400;          // the areas are written once and read once, at some 3400 bytes a clock
     if (cost < (S == 1 ? 1.0 : 0.97) * best_cost) { best = S; best_cost = cost; }
   }
-  const int per = (sh[count - 1].kblocks + best - 1) / best;                  // no empty slice
-  return (sh[count - 1].kblocks + per - 1) / per;
+  return best;
 }
