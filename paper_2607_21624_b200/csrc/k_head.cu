@@ -110,91 +110,113 @@ __global__ void __launch_bounds__(256) head_rows_kernel(const int32_t* __restric
     for (int p = 0; p < panels; ++p) to[p * pitch + (int64_t)c * 8] = make_uint4(0u, 0u, 0u, 0u);
 }
 
-// A teacher's top logits: their softmax over the ids given, ids given twice added up, sorted by id.  A warp has a row, a lane up
-// to four of its entries; every entry is compared with every other (K^2 broadcasts from shared memory: 4096 rows of 64 take about
-// the time that their 2 MB take to arrive).  Additions go in the order of the entries.  Ids below zero are not there, a row without
-// any, or whose logits are all -inf, carries no loss; ids past the vocabulary and logits of NaN or +inf make it NaN.
+// A teacher's top logits: their softmax over the ids given, ids given twice added up, sorted by id.  A warp has a row, a lane every
+// 32nd of its entries (PER of them, as top_k needs): keys of an id and the entry's place are sorted in registers by exchanges, so
+// that equal ids are neighbours, in the order of the list, and are added up in it.  Ids below zero are not there, a row without
+// any, or whose logits are all -inf, carries no loss; ids past the vocabulary and logits of NaN or +inf make it NaN.  The block's
+// eight rows leave through shared memory, eight values of an entry to a 32-byte sector.  Bound by instructions.  (Every entry compared
+// with every other, and a warp storing its own row's: 24.5 us for 4096 rows of 64.)
 constexpr int ENTRY_WARPS = 8;
+template <int PER>
 __global__ void __launch_bounds__(32 * ENTRY_WARPS) teacher_entries_kernel(const int32_t* __restrict__ ids, const float* __restrict__ logits,
                                                                            int top_k, float temperature, HeadRows R, int seq, int t_pad,
                                                                            int vocab, int32_t* status) {
-  constexpr int PER = HEAD_MAX_TOP / 32;
-  __shared__ int s_id[ENTRY_WARPS][HEAD_MAX_TOP];
-  __shared__ float s_p[ENTRY_WARPS][HEAD_MAX_TOP];
+  constexpr int N = 32 * PER;
+  constexpr uint32_t NO_KEY = 0xffffffffu;
+  static_assert(HEAD_MAX_TOP <= 128, "a key is an id times 128 and a place");
+  __shared__ float s_p[ENTRY_WARPS][N], s_y[N][ENTRY_WARPS];
+  __shared__ uint32_t s_key[ENTRY_WARPS][N];
+  __shared__ int s_id[N][ENTRY_WARPS], s_count[ENTRY_WARPS];
   pdl_launch_dependents();
   pdl_wait();
   start_pass(status);
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  const int row = blockIdx.x * ENTRY_WARPS + warp;
-  if (row >= R.rows) return;
+  const int row = blockIdx.x * ENTRY_WARPS + warp;             // rows come in eights
   const int b = row / t_pad, t = row - b * t_pad;
   const int64_t at = ((int64_t)b * seq + t) * top_k;
-  int id[PER];
+  uint32_t key[PER];
   float p[PER], top = -INFINITY;
   bool bad = false;
 #pragma unroll
   for (int j = 0; j < PER; ++j) {
     const int e = j * 32 + lane;
-    id[j] = t < seq && e < top_k ? ids[at + e] : -1;
-    p[j] = id[j] >= 0 ? logits[at + e] / temperature : -INFINITY;
-    bad = bad || id[j] >= vocab || p[j] != p[j];
+    const bool in = t < seq && e < top_k;
+    const int id = in ? ids[at + e] : -1;
+    const float z = in ? logits[at + e] : 0.f;
+    key[j] = id >= 0 ? (uint32_t)id * 128u + (uint32_t)e : NO_KEY;
+    p[j] = id >= 0 ? z / temperature : -INFINITY;
+    bad = bad || id >= vocab || p[j] != p[j];
     top = fmaxf(top, p[j]);
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
   bad = __any_sync(0xffffffffu, bad) || top == INFINITY;
-  if (bad || top == -INFINITY) {
-    if (lane == 0) { R.count[row] = bad ? -1 : 0; R.constant[row] = bad ? NAN : 0.f; }
-    return;
-  }
-  float sum = 0.f;
-#pragma unroll
-  for (int j = 0; j < PER; ++j) { p[j] = expf(p[j] - top); sum += p[j]; }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-#pragma unroll
-  for (int j = 0; j < PER; ++j) {
-    const int e = j * 32 + lane;
-    p[j] /= sum;
-    s_id[warp][e] = id[j];
-    s_p[warp][e] = p[j];
-  }
-  __syncwarp();
-  // an id's first entry takes the probability of all of them
-  bool first[PER];
-  float y[PER];
-#pragma unroll
-  for (int j = 0; j < PER; ++j) { first[j] = id[j] >= 0; y[j] = 0.f; }
-  for (int e = 0; e < top_k; ++e) {
-    const int other = s_id[warp][e];
-    const float q = s_p[warp][e];
-#pragma unroll
-    for (int j = 0; j < PER; ++j)
-      if (other == id[j]) { y[j] += q; first[j] = first[j] && e >= j * 32 + lane; }
-  }
-  __syncwarp();
-#pragma unroll
-  for (int j = 0; j < PER; ++j)
-    if (!first[j]) s_id[warp][j * 32 + lane] = headk::NONE;
-  __syncwarp();
-  int rank[PER] = {}, count = 0;
+  int count = 0;
   float constant = 0.f;
-  for (int e = 0; e < top_k; ++e) {
-    const int other = s_id[warp][e];
-    count += other != headk::NONE;
+  if (!bad && top > -INFINITY) {
+    float sum = 0.f;
 #pragma unroll
-    for (int j = 0; j < PER; ++j) rank[j] += other < id[j];
+    for (int j = 0; j < PER; ++j) { p[j] = expf(p[j] - top); sum += p[j]; }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+#pragma unroll
+    for (int j = 0; j < PER; ++j) s_p[warp][j * 32 + lane] = p[j] / sum;
+    // bitonic sort: key number i is key[i / 32] of lane i % 32
+#pragma unroll
+    for (int size = 2; size <= N; size *= 2)
+#pragma unroll
+      for (int d = size / 2; d > 0; d /= 2) {
+        if (d >= 32) {
+#pragma unroll
+          for (int j = 0; j < PER; ++j) {
+            if (j & (d / 32)) continue;
+            const bool up = ((j * 32) & size) == 0;
+            const uint32_t lo = min(key[j], key[(j + d / 32) % PER]), hi = max(key[j], key[(j + d / 32) % PER]);
+            key[j] = up ? lo : hi;
+            key[(j + d / 32) % PER] = up ? hi : lo;
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < PER; ++j) {
+            const uint32_t other = __shfl_xor_sync(0xffffffffu, key[j], d);
+            const bool up = ((j * 32 + lane) & size) == 0, low = (lane & d) == 0;
+            key[j] = up == low ? min(key[j], other) : max(key[j], other);
+          }
+        }
+      }
+#pragma unroll
+    for (int j = 0; j < PER; ++j) s_key[warp][j * 32 + lane] = key[j];
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const int i = j * 32 + lane;
+      const uint32_t id = key[j] / 128u;
+      const bool first = key[j] != NO_KEY && (i == 0 || s_key[warp][i - 1] / 128u != id);
+      const uint32_t firsts = __ballot_sync(0xffffffffu, first);
+      if (first) {                                             // takes the probability of the id's other places, too
+        float y = s_p[warp][key[j] % 128u];
+        for (int n = i + 1; n < N && s_key[warp][n] != NO_KEY && s_key[warp][n] / 128u == id; ++n) y += s_p[warp][s_key[warp][n] % 128u];
+        const int rank = count + __popc(firsts & ((1u << lane) - 1));
+        s_id[rank][warp] = (int)id;
+        s_y[rank][warp] = y;
+        if (y > 0.f) constant = fmaf(y, logf(y), constant);
+      }
+      count += __popc(firsts);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) constant += __shfl_xor_sync(0xffffffffu, constant, o);
   }
-#pragma unroll
-  for (int j = 0; j < PER; ++j) {
-    if (!first[j]) continue;
-    R.ids[(int64_t)rank[j] * R.rows + row] = id[j];
-    R.y[(int64_t)rank[j] * R.rows + row] = y[j];
-    if (y[j] > 0.f) constant = fmaf(y[j], logf(y[j]), constant);
+  if (lane == 0) {
+    R.count[row] = bad ? -1 : count;
+    R.constant[row] = bad ? NAN : constant;
+    s_count[warp] = count;
   }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) constant += __shfl_xor_sync(0xffffffffu, constant, o);
-  if (lane == 0) { R.count[row] = count; R.constant[row] = constant; }
+  __syncthreads();
+  const int r = threadIdx.x % ENTRY_WARPS, mine = s_count[r];
+  for (int e = threadIdx.x / ENTRY_WARPS; e < mine; e += 32) {
+    R.ids[(int64_t)e * R.rows + blockIdx.x * ENTRY_WARPS + r] = s_id[e][r];
+    R.y[(int64_t)e * R.rows + blockIdx.x * ENTRY_WARPS + r] = s_y[e][r];
+  }
 }
 
 // (k, s) stands for s 2^k.
@@ -374,8 +396,9 @@ cudaError_t launch_head_rows(int dtype, const int32_t* targets, const HeadRows& 
 }
 cudaError_t launch_teacher_entries(const int32_t* ids, const float* logits, int top_k, float temperature, const HeadRows& R, int seq, int t_pad,
                                    int vocab, int32_t* status, cudaStream_t st) {
-  return launch_pdl(teacher_entries_kernel, dim3((unsigned)((R.rows + ENTRY_WARPS - 1) / ENTRY_WARPS)), dim3(32 * ENTRY_WARPS), 0, st, ids, logits,
-                    top_k, temperature, R, seq, t_pad, vocab, status);
+  auto kernel = top_k <= 32 ? teacher_entries_kernel<1> : top_k <= 64 ? teacher_entries_kernel<2> : teacher_entries_kernel<4>;
+  return launch_pdl(kernel, dim3((unsigned)(R.rows / ENTRY_WARPS)), dim3(32 * ENTRY_WARPS), 0, st, ids, logits, top_k, temperature, R, seq, t_pad,
+                    vocab, status);
 }
 cudaError_t launch_head_combine(const float2* part, int tiles, const float* z_at, const HeadRows& R, float scale, float* loss, float* total,
                                 float* block_sums, int seq, int t_pad, int32_t* status, cudaStream_t st) {

@@ -4,7 +4,6 @@
 
 constexpr int HEAD_MAX_TOP = 128;       // teacher logits a token
 constexpr int HEAD_TICKET = 32;         // word of the status word's block in which head_combine_kernel counts its blocks
-namespace headk { constexpr int NONE = 0x7fffffff; }
 
 // What the forward keeps of the padded token rows, in `saved`.  The products run over the rows that carry a loss, in their order.
 struct HeadRows {
