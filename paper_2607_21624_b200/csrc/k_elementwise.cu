@@ -4,10 +4,33 @@
 // run of whole 128-byte lines.
 #include <math.h>
 
+#include <atomic>
+#include <mutex>
+
 #include "fbl_internal.h"
 #include "pdl.cuh"
 
 namespace {
+
+// The dynamic shared memory that a kernel has been allowed on each device, so that a launch asks for it once and not every time (a
+// microsecond of host work, of the six that a norm's backward takes).
+struct SmemLimit {
+  std::atomic<int> have[64] = {};
+  std::mutex lock;              // it only ever grows
+  template <typename Kernel>
+  cudaError_t raise(Kernel k, size_t bytes) {
+    int dev = -1;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const bool known = dev >= 0 && dev < 64;
+    if (known && have[dev].load(std::memory_order_relaxed) >= (int)bytes) return cudaSuccess;
+    std::lock_guard<std::mutex> hold(lock);
+    if (known && have[dev].load(std::memory_order_relaxed) >= (int)bytes) return cudaSuccess;
+    e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e == cudaSuccess && known) have[dev].store((int)bytes, std::memory_order_relaxed);
+    return e;
+  }
+};
 
 template <typename T> struct Vec16 { static constexpr int N = 16 / (int)sizeof(T); };
 
@@ -295,6 +318,98 @@ __global__ void __launch_bounds__(512) norm_fwd_kernel(const T* __restrict__ X, 
         }
       }
       rb += groups;
+    }
+  }
+}
+
+// The forward of the norm as an operator of its own, many wide rows: a warp has a row, up to NV vectors a lane, so that row sums are
+// shuffles and nothing waits for another warp.  Its next rows are on their way to a ring of its own in shared memory, in which every lane
+// reads back what it copied itself: twelve warps keep about 100 KB of an SM's on the way, what memory takes (6.55 TB/s x some 2 us
+// over 148 SMs: 90 KB), while others compute and store.  gamma and beta come from shared memory.  The kernel above lets 256 threads share
+// such a row, behind a barrier a row sum.
+constexpr int ROWS_WARPS = 12;
+__host__ __device__ constexpr int rows_stages(int nv) { return nv > 8 ? 2 : nv > 4 ? 4 : 8; }
+template <typename T, int NV>
+__global__ void __launch_bounds__(32 * ROWS_WARPS, 1) norm_rows_kernel(const T* __restrict__ X, const float* __restrict__ gamma, const float* __restrict__ beta,
+                                                           T* __restrict__ Y, float* __restrict__ stats, int64_t n_pad, int d, int seq, int t_pad,
+                                                           int rms, float eps, int32_t* __restrict__ status) {
+  constexpr int V = Vec16<T>::N, TW = tile_w_of<T>::value;
+  constexpr int S = rows_stages(NV);
+  extern __shared__ __align__(16) float s_params[];           // gamma, beta; the warps' rings [stage][vector][lane]
+  if (blockIdx.x == 0 && threadIdx.x == 0) *status = 0;
+  pdl_launch_dependents();
+  for (int c = threadIdx.x; c < d; c += 32 * ROWS_WARPS) {    // inputs of the step, as above
+    s_params[c] = gamma[c];
+    if (beta) s_params[d + c] = beta[c];
+  }
+  __syncthreads();
+  pdl_wait();
+  const int lane = threadIdx.x % 32, nvec = d / V;
+  const float inv_d = 1.f / (float)d;
+  const uint4* ring = reinterpret_cast<const uint4*>(s_params + (beta ? 2 : 1) * d) + threadIdx.x / 32 * (S * NV * 32) + lane;
+  const uint32_t ring_addr = (uint32_t)__cvta_generic_to_shared(ring);
+  const int64_t step = (int64_t)gridDim.x * ROWS_WARPS;
+  auto fetch = [&](int64_t r, int stage) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int v = lane + 32 * j;
+      const bool live = v < nvec && r < n_pad;
+      cp_async16(ring_addr + (stage * NV + j) * 512, X + (live ? ((int64_t)(v / 8) * n_pad + r) * TW + (v % 8) * V : 0), live);
+    }
+    cp_async_commit();
+  };
+  int64_t r = (int64_t)blockIdx.x * ROWS_WARPS + threadIdx.x / 32;
+#pragma unroll
+  for (int i = 0; i < S - 1; ++i) fetch(r + i * step, i);
+  for (int stage = 0; r < n_pad; r += step, stage = stage == S - 1 ? 0 : stage + 1) {
+    fetch(r + (S - 1) * step, stage == 0 ? S - 1 : stage - 1);        // the stage read a row ago
+    cp_async_wait<S - 1>();
+    const bool pad = (int)(r % t_pad) >= seq;
+    uint4 x[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) x[j] = ring[(stage * NV + j) * 32];
+    float mean = 0.f;
+    float2 t = both(0.f);
+    if (!rms) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) t = __fadd2_rn(t, pair_of<T>(x[j], i));
+      mean = t.x + t.y;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) mean += __shfl_xor_sync(0xffffffffu, mean, o);
+      mean *= inv_d;
+    }
+    const float2 shift = both(-mean);
+    t = both(0.f);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      if (lane + 32 * j >= nvec) continue;
+#pragma unroll
+      for (int i = 0; i < V / 2; ++i) {
+        const float2 c = __fadd2_rn(pair_of<T>(x[j], i), shift);
+        t = __ffma2_rn(c, c, t);
+      }
+    }
+    float q = t.x + t.y;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) q += __shfl_xor_sync(0xffffffffu, q, o);
+    const float rstd = rsqrtf(q * inv_d + eps);
+    if (lane == 0) *reinterpret_cast<float2*>(stats + 2 * r) = pad ? make_float2(0.f, 0.f) : make_float2(mean, rstd);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int v = lane + 32 * j;
+      if (v >= nvec) continue;
+      float2 y[V / 2];
+#pragma unroll
+      for (int i = 0; i < V / 2; i += 2) {
+        const float4 g = *reinterpret_cast<const float4*>(s_params + v * V + 2 * i);
+        const float4 b = beta ? *reinterpret_cast<const float4*>(s_params + d + v * V + 2 * i) : make_float4(0.f, 0.f, 0.f, 0.f);
+        const float2 c0 = __fmul2_rn(__fadd2_rn(pair_of<T>(x[j], i), shift), both(rstd)), c1 = __fmul2_rn(__fadd2_rn(pair_of<T>(x[j], i + 1), shift), both(rstd));
+        y[i] = pad ? both(0.f) : __ffma2_rn(c0, make_float2(g.x, g.y), make_float2(b.x, b.y));
+        y[i + 1] = pad ? both(0.f) : __ffma2_rn(c1, make_float2(g.z, g.w), make_float2(b.z, b.w));
+      }
+      store_pairs(Y + ((int64_t)(v / 8) * n_pad + r) * TW + (v % 8) * V, y);
     }
   }
 }
@@ -794,7 +909,8 @@ cudaError_t norm_bwd_launch(const fbl_plan* p, const NormShape& s, const void* d
   }
   const size_t sums = (size_t)s.groups * 2 * s.tpr * NV * V * sizeof(float), smem = ring > sums ? ring : sums;
   cudaError_t e = cudaSuccess;
-  if (smem > 40 * 1024) e = cudaFuncSetAttribute(norm_bwd_kernel<T, NV, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  static SmemLimit limit;
+  if (smem > 40 * 1024) e = limit.raise(norm_bwd_kernel<T, NV, R>, smem);
   if (e != cudaSuccess) return e;
   e = launch_pdl(norm_bwd_kernel<T, NV, R>, dim3(blocks + cs_blocks), dim3(s.tpr * s.groups), smem, st,
                              (const T*)dXn, (const T*)X, (const T*)dY, stats, gamma, (T*)dX, dgamma ? part : (float*)nullptr, p->n_pad,
@@ -888,6 +1004,30 @@ cudaError_t launch_rope_bwd_round(const fbl_plan* p, const float* acc, void* dQ,
   const int blocks = (int)min((int64_t)p->sm_count * 16, (total + 255) / 256);
   return launch_pdl(rope_bwd_round_kernel, dim3(blocks), dim3(256), 0, st, acc, (__nv_bfloat16*)dQ, p->d.n_q_heads, (__nv_bfloat16*)dK,
                     p->d.n_kv_heads, p->n_pad, p->d.seq, p->t_pad, p->d.head_dim, rope);
+}
+
+template <typename T, int NV>
+cudaError_t norm_rows_launch(const fbl_plan* p, const void* X, const float* gamma, const float* beta, void* Y, float* stats, int32_t* status, cudaStream_t st) {
+  static SmemLimit limit;
+  const unsigned blocks = (unsigned)min((int64_t)p->sm_count, (p->n_pad + ROWS_WARPS - 1) / ROWS_WARPS);
+  const size_t smem = (size_t)p->d.d_model * sizeof(float) * (beta ? 2 : 1) + (size_t)ROWS_WARPS * rows_stages(NV) * NV * 512;
+  const cudaError_t e = limit.raise(norm_rows_kernel<T, NV>, smem);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(norm_rows_kernel<T, NV>, dim3(blocks), dim3(32 * ROWS_WARPS), smem, st, (const T*)X, gamma, beta, (T*)Y, stats,
+                    p->n_pad, p->d.d_model, p->d.seq, p->t_pad, (int)(p->d.norm == FBL_NORM_RMSNORM), p->d.eps, status);
+}
+cudaError_t launch_norm_op_fwd(const fbl_plan* p, const void* X, const float* gamma, const float* beta, void* Y, float* stats, int32_t* status,
+                               cudaStream_t st) {
+  if (p->d.norm == FBL_NORM_RMSNORM) beta = nullptr;
+  const int nvec = p->d.d_model / (p->d.dtype == FBL_DTYPE_FP32 ? 4 : 8);
+  // (us, a block a row and a warp a row)  fp32: 592 x 2048 4.6, 5.6; 1665 x 1280 9.8, 6.0; 8192 x 2048 35.8, 26.0.  bf16, with twice the
+  // instructions a byte: 16384 x 1024 17.7, 20.0; 4096 x 2048 9.7, 10.2; 1184 x 4096 7.1, 7.7; 8192 x 4096 32.1, 28.0 (LayerNorm 35.6, 33.7)
+  const bool fp32 = p->d.dtype == FBL_DTYPE_FP32;
+  if (nvec > 512 || nvec <= (fp32 ? 96 : 384) || p->n_pad < (fp32 ? 8 : 24) * (int64_t)p->sm_count)
+    return launch_norm_fwd(p, X, gamma, beta, Y, stats, status, st);
+  if (!fp32) return norm_rows_launch<__nv_bfloat16, 16>(p, X, gamma, beta, Y, stats, status, st);
+  return nvec <= 128 ? norm_rows_launch<float, 4>(p, X, gamma, beta, Y, stats, status, st) : nvec <= 256 ? norm_rows_launch<float, 8>(p, X, gamma, beta, Y, stats, status, st)
+         : nvec <= 384 ? norm_rows_launch<float, 12>(p, X, gamma, beta, Y, stats, status, st) : norm_rows_launch<float, 16>(p, X, gamma, beta, Y, stats, status, st);
 }
 
 cudaError_t launch_norm_fwd(const fbl_plan* p, const void* X, const float* gamma, const float* beta, void* Xn,

@@ -51,7 +51,10 @@ class HeadPlan:
     def __init__(self, desc: FblHeadDesc):
         self._h = C.c_void_p()
         self.desc = desc
-        _check(_bind().fbl_head_plan_create(C.byref(desc), C.byref(self._h)))
+        L = _bind()
+        _check(L.fbl_head_plan_create(C.byref(desc), C.byref(self._h)))
+        # looked up once: a call of a few tokens is host work
+        self._xent_fwd, self._distill_fwd, self._bwd = L.fbl_head_xent_fwd, L.fbl_head_distill_fwd, L.fbl_head_bwd
 
     def close(self):
         if self._h:
@@ -81,14 +84,20 @@ class HeadPlan:
         _check(lib().fbl_head_unpack(self._h, matrix_id, tiled_ptr, rowmajor_ptr, stream))
 
     def xent_fwd(self, X, W, targets, loss, total, saved, scratch, stream):
-        _check(lib().fbl_head_xent_fwd(self._h, X, W, targets, loss, total, saved, scratch, stream))
+        code = self._xent_fwd(self._h, X, W, targets, loss, total, saved, scratch, stream)
+        if code:
+            _check(code)
 
     def distill_fwd(self, X, W, top_ids, top_logits, loss, total, saved, scratch, stream):
-        _check(lib().fbl_head_distill_fwd(self._h, X, W, top_ids, top_logits, loss, total, saved, scratch, stream))
+        code = self._distill_fwd(self._h, X, W, top_ids, top_logits, loss, total, saved, scratch, stream)
+        if code:
+            _check(code)
 
     def bwd(self, X, W, dloss, saved, dX, dW, scratch, stream):
         """dloss None: the gradient of the mean loss.  dX or dW None: not formed."""
-        _check(lib().fbl_head_bwd(self._h, X, W, dloss, saved, dX, dW, scratch, stream))
+        code = self._bwd(self._h, X, W, dloss, saved, dX, dW, scratch, stream)
+        if code:
+            _check(code)
 
     def status_poll(self, scratch) -> int:
         out = C.c_int32()

@@ -44,7 +44,10 @@ class NormPlan:
     def __init__(self, desc: FblNormDesc):
         self._h = C.c_void_p()
         self.desc = desc
-        _check(_bind().fbl_norm_plan_create(C.byref(desc), C.byref(self._h)))
+        L = _bind()
+        _check(L.fbl_norm_plan_create(C.byref(desc), C.byref(self._h)))
+        # looked up once: a call of a few tokens is host work
+        self._fwd, self._bwd = L.fbl_norm_fwd, L.fbl_norm_bwd
 
     def close(self):
         if self._h:
@@ -74,11 +77,15 @@ class NormPlan:
         _check(lib().fbl_norm_unpack(self._h, tiled_ptr, rowmajor_ptr, stream))
 
     def fwd(self, X, gamma, beta, Y, saved, scratch, stream):
-        _check(lib().fbl_norm_fwd(self._h, X, gamma, beta, Y, saved, scratch, stream))
+        code = self._fwd(self._h, X, gamma, beta, Y, saved, scratch, stream)
+        if code:
+            _check(code)
 
     def bwd(self, dY, X, gamma, saved, dX, dgamma, dbeta, scratch, stream):
         """dgamma and dbeta None: the norm's parameters are frozen."""
-        _check(lib().fbl_norm_bwd(self._h, dY, X, gamma, saved, dX, dgamma, dbeta, scratch, stream))
+        code = self._bwd(self._h, dY, X, gamma, saved, dX, dgamma, dbeta, scratch, stream)
+        if code:
+            _check(code)
 
     def launch_count(self) -> int:
         return lib().fbl_norm_launch_count(self._h)

@@ -433,7 +433,8 @@ def test_weights_beyond_32_bit_offsets():
 
 @pytest.mark.parametrize("norm", ["layernorm", "rmsnorm"])
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
-@pytest.mark.parametrize("shape", [(1, 1, 64), (1, 1, 768), (3, 5, 128), (2, 197, 320), (7, 13, 1088), (1, 600, 2048), (2, 9, 16384)],
+@pytest.mark.parametrize("shape", [(1, 1, 64), (1, 1, 768), (3, 5, 128), (2, 197, 320), (7, 13, 1088), (1, 600, 2048), (2, 9, 16384), (3, 399, 448),
+                                   (1, 1190, 1280), (2, 595, 960), (1, 1184, 2048), (1, 3561, 4096), (2, 1777, 3584)],
                          ids=lambda s: "x".join(map(str, s)))
 def test_norm(shape, dtype, norm):
     c = cfg(*shape, 8, dtype, norm=norm)
