@@ -160,7 +160,7 @@ __device__ __forceinline__ bool head_stats_tile(const Problem& P, int m0, int n0
     headepi::load_panel(acc, pn, v);
     headepi::stats64(H, R, v, n0 + pn * 64, k, s);
   }
-  if (R.live) H.part[(long long)m * H.tiles + n0 / HEAD_TILE] = make_float2(k, s);
+  if (R.live) H.part[(long long)R.row * H.tiles + n0 / HEAD_TILE] = make_float2(k, s);
   return true;
 }
 

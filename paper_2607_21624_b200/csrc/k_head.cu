@@ -219,74 +219,94 @@ __global__ void __launch_bounds__(32 * ENTRY_WARPS) teacher_entries_kernel(const
   }
 }
 
-// (k, s) stands for s 2^k.
-__device__ __forceinline__ void join(float& k, float& s, float k2, float s2) {
-  const float top = fmaxf(k, k2);
-  s = (k == top ? s : s * exp2f(k - top)) + (k2 == top ? s2 : s2 * exp2f(k2 - top));
-  k = top;
-}
+// s 2^k in units of 2^top, where k is at most top; nothing where nothing has been added up (k = -inf: of two such, -inf - -inf is NaN).
+__device__ __forceinline__ float scaled(float k, float s, float top) { return k == top ? s : s * exp2f(k - top); }
 
-// A warp has a row: its lanes share the row's partials, which lie behind each other, and its entries; all joins and sums go in a fixed
-// order.  loss = sum of y (log y - logit) + log of the sum of exp(logit).  The block that ends last adds the blocks' sums up.  What
-// bounds it is latency: a row's values, its partials and its entries are three loads behind each other, and the blocks' sums two more.
-__global__ void __launch_bounds__(256) head_combine_kernel(const float2* __restrict__ part, int tiles, const float* __restrict__ z_at,
-                                                           HeadRows R, float scale, float* __restrict__ loss, float* __restrict__ total,
-                                                           float2* __restrict__ block_sums, int seq, int t_pad, int32_t* status) {
-  __shared__ float2 s_row[8];
-  __shared__ double s_sum[8], s_count[8];
+// A warp has a row at a time: its lanes share the row's partials, which lie behind each other, and its entries; all joins and sums go in
+// a fixed order.  loss = sum of y (log y - logit) + log of the sum of exp(logit).  What bounds it is latency, so all that a row needs is
+// asked for at once (of rows without a loss, too, whose partials are nothing), and up to 64 rows are one block's, which adds its
+// losses up itself; of several blocks the one that ends last does, two latencies later.
+constexpr int COMBINE_FEW = 64;
+__global__ void __launch_bounds__(1024) head_combine_kernel(const float2* __restrict__ part, int tiles, const float* __restrict__ z_at,
+                                                            HeadRows R, float scale, float* __restrict__ loss, float* __restrict__ total,
+                                                            float2* __restrict__ block_sums, int seq, int t_pad, int32_t* status) {
+  constexpr int U = 8;
+  __shared__ double s_sum[32], s_count[32];
   __shared__ int s_last;
   pdl_launch_dependents();
   pdl_wait();
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, row = blockIdx.x * 8 + warp;      // rows come in eights
-  const int pos = R.pos[row], count = R.count[row];
-  const float constant = R.constant[row];
-  float l = 0.f;
-  if (pos >= 0) {
-    float k = -INFINITY, s = 0.f;
-    const float2* mine = part + (int64_t)pos * tiles;
-#pragma unroll 1
-    for (int t0 = 0; t0 < tiles; t0 += 256) {
-      float2 v[8];
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, warps = blockDim.x / 32;
+  double sum = 0.0, counted = 0.0;
+  for (int row = blockIdx.x * warps + warp; row < R.rows; row += gridDim.x * warps) {
+    const float2* mine = part + (int64_t)row * tiles;
+    float2 v[U];
+    auto load = [&](int t0) {
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
+      for (int u = 0; u < U; ++u) {
         const int t = t0 + 32 * u + lane;
         v[u] = t < tiles ? __ldcg(mine + t) : make_float2(-INFINITY, 0.f);
       }
+    };
+    load(0);
+    const float y0 = R.y[row], z0 = __ldcg(z_at + row), constant = R.constant[row];      // entry 0, which lane 0 takes
+    const int count = R.count[row];
+    float l = 0.f;
+    if (count != 0) {
+      float k = -INFINITY, s = 0.f;
+#pragma unroll 1
+      for (int t0 = 0;;) {
+        float top = v[0].x, some = 0.f;                        // the largest first: the exponentials then do not wait for one another
 #pragma unroll
-      for (int u = 0; u < 8; ++u) join(k, s, v[u].x, v[u].y);
-    }
+        for (int u = 1; u < U; ++u) top = fmaxf(top, v[u].x);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      const float k2 = __shfl_xor_sync(0xffffffffu, k, o), s2 = __shfl_xor_sync(0xffffffffu, s, o);
-      join(k, s, k2, s2);
-    }
-    float toward = 0.f;                     // sum of y (k - c z)
-    for (int e = lane; e < count; e += 32) {
-      const float y = R.y[(int64_t)e * R.rows + row], z = __ldcg(z_at + (int64_t)e * R.rows + row);
-      if (y != 0.f) toward = fmaf(y, -fmaf(z, scale, -k), toward);
-    }
+        for (int u = 0; u < U; ++u) some += scaled(v[u].x, v[u].y, top);
+        const float both = fmaxf(k, top);
+        s = scaled(k, s, both) + scaled(top, some, both);
+        k = both;
+        if ((t0 += 32 * U) >= tiles) break;
+        load(t0);
+      }
+      float top = k;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) toward += __shfl_xor_sync(0xffffffffu, toward, o);
-    l = count < 0 ? NAN : fmaf(LN2, toward, logf(s)) + constant;
-    if (lane == 0) { R.k[row] = k; R.sum[row] = s; }
-  }
-  if (lane == 0) {
+      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      s = scaled(k, s, top);
+      k = top;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+      float toward = 0.f;                   // sum of y (k - c z)
+      for (int e = lane; e < count; e += 32) {
+        const float y = e ? R.y[(int64_t)e * R.rows + row] : y0, z = e ? __ldcg(z_at + (int64_t)e * R.rows + row) : z0;
+        if (y != 0.f) toward = fmaf(y, -fmaf(z, scale, -k), toward);
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) toward += __shfl_xor_sync(0xffffffffu, toward, o);
+      l = count < 0 ? NAN : fmaf(LN2, toward, logf(s)) + constant;
+      if (lane == 0) { R.k[row] = k; R.sum[row] = s; }
+      sum += l;
+      counted += 1.0;
+    }
     const int b = row / t_pad, t = row - b * t_pad;
-    if (t < seq) loss[(int64_t)b * seq + t] = l;
-    s_row[warp] = make_float2(l, count != 0 ? 1.f : 0.f);
+    if (lane == 0 && t < seq) loss[(int64_t)b * seq + t] = l;
   }
+  if (lane == 0) { s_sum[warp] = sum; s_count[warp] = counted; }
   __syncthreads();
-  float2 sum = make_float2(0.f, 0.f);
+  auto whole = [&](double& a, double& n) {                     // by thread 0
+    a = n = 0.0;
+    for (int w = 0; w < warps; ++w) { a += s_sum[w]; n += s_count[w]; }
+  };
+  auto publish = [&](double a, double n) {
+    total[0] = R.total[0] = (float)a;
+    total[1] = R.total[1] = (float)n;
+  };
   if (threadIdx.x == 0) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) { sum.x += s_row[i].x; sum.y += s_row[i].y; }
-    if (gridDim.x > 1) {
-      block_sums[blockIdx.x] = sum;
+    double a, n;
+    whole(a, n);
+    if (gridDim.x == 1) {
+      publish(a, n);
+    } else {
+      block_sums[blockIdx.x] = make_float2((float)a, (float)n);
       __threadfence();
       s_last = atomicAdd(status + HEAD_TICKET, 1) == (int)gridDim.x - 1;
-    } else {
-      total[0] = R.total[0] = sum.x;
-      total[1] = R.total[1] = sum.y;
     }
   }
   if (gridDim.x == 1) return;
@@ -295,7 +315,7 @@ __global__ void __launch_bounds__(256) head_combine_kernel(const float2* __restr
   __threadfence();
   double a = 0.0, n = 0.0;
 #pragma unroll 4
-  for (int i = threadIdx.x; i < (int)gridDim.x; i += 256) {
+  for (int i = threadIdx.x; i < (int)gridDim.x; i += blockDim.x) {
     const float2 v = __ldcg(block_sums + i);
     a += v.x;
     n += v.y;
@@ -308,11 +328,8 @@ __global__ void __launch_bounds__(256) head_combine_kernel(const float2* __restr
   if (lane == 0) { s_sum[warp] = a; s_count[warp] = n; }
   __syncthreads();
   if (threadIdx.x == 0) {
-    a = n = 0.0;
-#pragma unroll
-    for (int w = 0; w < 8; ++w) { a += s_sum[w]; n += s_count[w]; }
-    total[0] = R.total[0] = (float)a;
-    total[1] = R.total[1] = (float)n;
+    whole(a, n);
+    publish(a, n);
   }
 }
 
@@ -402,7 +419,8 @@ cudaError_t launch_teacher_entries(const int32_t* ids, const float* logits, int 
 }
 cudaError_t launch_head_combine(const float2* part, int tiles, const float* z_at, const HeadRows& R, float scale, float* loss, float* total,
                                 float* block_sums, int seq, int t_pad, int32_t* status, cudaStream_t st) {
-  return launch_pdl(head_combine_kernel, dim3((unsigned)(R.rows / 8)), dim3(256), 0, st, part, tiles, z_at, R, scale, loss, total, (float2*)block_sums, seq,
+  const bool few = R.rows <= COMBINE_FEW;
+  return launch_pdl(head_combine_kernel, dim3(few ? 1u : (unsigned)(R.rows / 8)), dim3(few ? (unsigned)R.rows / 8 * 128 : 256), 0, st, part, tiles, z_at, R, scale, loss, total, (float2*)block_sums, seq,
                     t_pad, status);
 }
 cudaError_t launch_head_scatter(int dtype, int sm_count, const float* acc, int areas, const HeadRows& R, int d_model, const float* over, float alpha,

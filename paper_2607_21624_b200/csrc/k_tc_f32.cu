@@ -360,7 +360,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_tc_f32_kernel(const __grid_co
       if constexpr (EPI == F32_HEAD_STATS) {
         float k = -INFINITY, s = 0.f;
         headepi::stats64(P.head, R, v, half_n, k, s);
-        if (R.live) P.head.part[(long long)half_m * P.head.tiles + half_n / HEAD_TILE_F32] = make_float2(k, s);
+        if (R.live) P.head.part[(long long)R.row * P.head.tiles + half_n / HEAD_TILE_F32] = make_float2(k, s);
       } else {
         headepi::grad64(P.head, R, v, P.head.col0 + half_n);
 #pragma unroll
