@@ -109,7 +109,7 @@ struct HeadEpi {
   long long rows;               // pitch of every per-row array here
   int vocab, col0;              // columns of the vocabulary, and the first one of this product's
   float scale;                  // from a product to a logit times log2 e
-  float2* part;                 // forward: [row][column tile, `tiles` of them] (k, sum of 2^(logit - k))
+  float2* part;                 // forward: [row][column tile, `tiles` of them] (k, sum of 2^((product - k) scale))
   int tiles;
   float* z_at;                  // forward: [entry][row] the products at the targets
   const float *k, *sum;         // backward: the row's k and sum

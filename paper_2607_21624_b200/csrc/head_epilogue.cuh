@@ -2,12 +2,12 @@
 // or as the gradient of their cross entropy (backward), so that no logit reaches memory.
 //
 // With z the product x.w of a token and a vocabulary column and c = log2 e / temperature,
-//   forward   k = round(c max z),  s = sum of 2^(c z - k)  over a tile's 256 columns, and z itself at the row's targets
-//   backward  dz = (g / s) 2^(c z - k) - g y,  g = the loss's gradient / temperature, y the target probability of the column
+//   forward   k = max z,  s = sum of 2^(c (z - k))  over a tile's columns, and z itself at the row's targets
+//   backward  dz = (g / s) 2^(c (z - k)) - g y,  g = the loss's gradient / temperature, y the target probability of the column
 //             (bf16: g = 1 for the mean loss, whose 1 / (tokens x temperature) the two products behind are scaled by: with it in dz every
 //             token's target would be rounded the same way, and dX and dW come out too large or too small by up to 2^-9)
-// k and s are a whole row's by then (head_combine_kernel).  c z - k is one multiply-add with the same c and k everywhere, so the
-// rounding of k cancels: a target that holds all of its row's probability gives log s = log 1 exactly.  Sums are fp32; dz is
+// k and s are a whole row's by then (head_combine_kernel).  Logits only ever enter as distances from the row's largest: a target that
+// holds all of its row's probability gives log s = log 1 exactly, and logits of any size have a loss.  Sums are fp32; dz is
 // rounded to the storage type, as an operand of the two products that consume it (bf16: half a step of 2^-8 of each value, as
 // large as the rounding of the results).
 //
@@ -107,16 +107,16 @@ __device__ __forceinline__ void stats64(const HeadEpi& H, Row<false>& R, uint32_
 #pragma unroll
     for (int i = 0; i < 4; ++i) top[i] = tc::fmax3(top[i], __uint_as_float(v[j + i]), __uint_as_float(v[j + 4 + i]));
   const float was = k;
-  k = fmaxf(k, tc::fmax3(top[0], top[1], fmaxf(top[2], top[3])) * H.scale);
+  k = fmaxf(k, tc::fmax3(top[0], top[1], fmaxf(top[2], top[3])));
   const float2 mk = make_float2(-k, -k), c2 = make_float2(H.scale, H.scale);
   float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
   for (int j = 0; j < 64; j += 2) {
-    const float2 x = __ffma2_rn(make_float2(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), c2, mk);
+    const float2 x = __fmul2_rn(__fadd2_rn(make_float2(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), mk), c2);
     sum[j / 2 % 2] = __fadd2_rn(sum[j / 2 % 2], make_float2(tc::fast_exp2(x.x), tc::fast_exp2(x.y)));
   }
   sum[0] = __fadd2_rn(sum[0], sum[1]);
-  s = s * tc::fast_exp2(was - k) + (sum[0].x + sum[0].y);
+  s = s * tc::fast_exp2((was - k) * H.scale) + (sum[0].x + sum[0].y);
 }
 
 // 64 columns of logits become their gradient.
@@ -124,7 +124,7 @@ __device__ __forceinline__ void grad64(const HeadEpi& H, Row<true>& R, uint32_t 
   const float2 c2 = make_float2(H.scale, H.scale), mk = make_float2(-R.k, -R.k), gs2 = make_float2(R.gs, R.gs);
 #pragma unroll
   for (int j = 0; j < 64; j += 2) {
-    const float2 x = __ffma2_rn(make_float2(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), c2, mk);
+    const float2 x = __fmul2_rn(__fadd2_rn(make_float2(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), mk), c2);
     const float2 d = __fmul2_rn(make_float2(tc::fast_exp2(x.x), tc::fast_exp2(x.y)), gs2);
     v[j] = __float_as_uint(d.x);
     v[j + 1] = __float_as_uint(d.y);

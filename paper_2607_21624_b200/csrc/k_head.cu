@@ -219,8 +219,9 @@ __global__ void __launch_bounds__(32 * ENTRY_WARPS) teacher_entries_kernel(const
   }
 }
 
-// s 2^k in units of 2^top, where k is at most top; nothing where nothing has been added up (k = -inf: of two such, -inf - -inf is NaN).
-__device__ __forceinline__ float scaled(float k, float s, float top) { return k == top ? s : s * exp2f(k - top); }
+// s 2^(c k) in units of 2^(c top), where k is at most top; nothing where nothing has been added up (k = -inf: of two such, -inf - -inf
+// is NaN).
+__device__ __forceinline__ float scaled(float k, float s, float top, float c) { return k == top ? s : s * exp2f((k - top) * c); }
 
 // A warp has a row at a time: its lanes share the row's partials, which lie behind each other, and its entries; all joins and sums go in
 // a fixed order.  loss = sum of y (log y - logit) + log of the sum of exp(logit).  What bounds it is latency, so all that a row needs is
@@ -259,9 +260,9 @@ __global__ void __launch_bounds__(1024) head_combine_kernel(const float2* __rest
 #pragma unroll
         for (int u = 1; u < U; ++u) top = fmaxf(top, v[u].x);
 #pragma unroll
-        for (int u = 0; u < U; ++u) some += scaled(v[u].x, v[u].y, top);
+        for (int u = 0; u < U; ++u) some += scaled(v[u].x, v[u].y, top, scale);
         const float both = fmaxf(k, top);
-        s = scaled(k, s, both) + scaled(top, some, both);
+        s = scaled(k, s, both, scale) + scaled(top, some, both, scale);
         k = both;
         if ((t0 += 32 * U) >= tiles) break;
         load(t0);
@@ -269,14 +270,14 @@ __global__ void __launch_bounds__(1024) head_combine_kernel(const float2* __rest
       float top = k;
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-      s = scaled(k, s, top);
+      s = scaled(k, s, top, scale);
       k = top;
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-      float toward = 0.f;                   // sum of y (k - c z)
+      float toward = 0.f;                   // sum of y c (k - z)
       for (int e = lane; e < count; e += 32) {
         const float y = e ? R.y[(int64_t)e * R.rows + row] : y0, z = e ? __ldcg(z_at + (int64_t)e * R.rows + row) : z0;
-        if (y != 0.f) toward = fmaf(y, -fmaf(z, scale, -k), toward);
+        if (y != 0.f) toward = fmaf(y, (k - z) * scale, toward);
       }
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) toward += __shfl_xor_sync(0xffffffffu, toward, o);

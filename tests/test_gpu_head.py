@@ -299,6 +299,42 @@ def test_confident_and_large_logits(dtype, tied):
     compare(c, inp, run, ref)
 
 
+@pytest.mark.parametrize("tied", [False, True], ids=["dv", "vd"])
+def test_fp32_operands_beyond_the_parts_range(monkeypatch, tied):
+    """Hidden states of 2^100 and weights of 2^97, whose products and gradients leave the range that operands in parts have: their tiles
+    are formed by multiply-adds, and the others are what they are without them."""
+    monkeypatch.setenv("FBL_HEAD_PIECE", "512")
+    c = cfg(2, 150, 128, 1339, "fp32", tied)
+    inp = make_head_inputs(c, ignored=0.2)
+    plain = HeadRunner(c)
+    plain.load_inputs(inp)
+    plain.step()
+    big = dict(inp, X=inp["X"].copy(), W=inp["W"].copy())
+    ref = orc.head_fwd_bwd(c, inp)
+    rows = np.argwhere(ref["has"])[[3, 170]]
+    for b, t in rows:
+        big["X"][b, t] *= 2.0 ** 100
+    ref = orc.head_fwd_bwd(c, big)
+    run = HeadRunner(c, guard_bytes=4096)
+    run.load_inputs(big)
+    run.step()
+    assert run.status() == 0 and run.guards_intact() == []
+    loss, want = run.fetch("loss").reshape(2, 150), ref["loss"]
+    assert np.isfinite(loss).all() and (np.abs(loss - want) <= 1e-5 * np.abs(want) + 1e-5).all()
+    dX = run.fetch("dX")
+    assert np.isfinite(dX).all() and fp32_err(dX, ref["dX"]) <= 1e-5
+    # dW is sums of 2^100 dz of those tokens: to fp32 steps of its terms
+    x = np.abs(big["X"].reshape(300, -1))
+    terms = x.T @ np.abs(ref["dZ"])
+    dW = run.fetch("dW")
+    assert (np.abs(dW - ref["dW"]) <= 1e-5 * (terms.T if tied else terms) + 1e-30).all()
+    # the other tokens' losses and gradients have not moved
+    same = np.ones((2, 150), dtype=bool)
+    same[rows[:, 0], rows[:, 1]] = False
+    assert np.abs(loss - plain.fetch("loss").reshape(2, 150))[same].max() <= 1e-5
+    assert fp32_err(dX[same], plain.fetch("dX")[same]) <= 1e-5
+
+
 def test_bits_repeat_on_dirty_work_areas():
     for c in (cfg(2, 300, 256, 5003, tied=True), cfg(4, 77, 128, 1500, top_k=32, tau=2.0), cfg(2, 150, 128, 1500, "fp32")):
         inp = make_head_inputs(c, ignored=0.3)
