@@ -29,21 +29,28 @@ struct alignas(64) Problem {
   const float* b[MAX_TERMS];
   long long a_rpad[MAX_TERMS], b_rpad[MAX_TERMS];
   int k[MAX_TERMS];
-  int b_rows[MAX_TERMS];                    // stored rows of B
-  // the reduction cut into `areas` ranges, work units of their own, whose sums go to a copy of C each, area_stride floats apart
-  int areas;
-  long long area_stride;
-  HeadEpi head;                             // of the vocabulary's products (epilogues 6 and 7)
-  int dyn;                                  // 1: G.rows rows instead of m, 2: a reduction over G.rows (GemmArgs)
 };
 struct alignas(64) Group {
   Problem p[MAX_PROBLEMS];
   int from[MAX_PROBLEMS];                           // which of the caller's problems each is
   int count, slices, reset_status;
   int32_t* status;
-  const int32_t* rows;
   uint4* zero_ptr;                                  // chores of the launch, see GemmArgs
   long long zero_vec;
+};
+
+// What the head's launches have besides (kernel variants of their own).
+struct HeadProblem {
+  int dyn;                                          // 1: rows counted by `rows` instead of m, 2: a reduction over them (GemmArgs)
+  // the reduction cut into `areas` ranges, work units of their own, whose sums go to a copy of C each, area_stride floats apart
+  int areas;
+  long long area_stride;
+  int m_stored, b_rows;                             // rows of C that are stored, and that B has
+};
+struct alignas(64) HeadGroup : Group {
+  HeadProblem h[2];
+  HeadEpi epi;
+  const int32_t* rows;
 };
 
 // Problems in the order of their reductions' lengths: the blocks that take longest start first.
@@ -62,7 +69,7 @@ inline bool fill_group(Group& G, const GemmArgs* gs, int count, const int* order
   for (int i = 0; i < count; ++i) {
     const GemmArgs& g = gs[G.from[i] = order[i]];
     Problem& P = G.p[i];
-    P.n_terms = g.n_terms; P.m = g.c_rows ? (int)g.c_rows : g.m; P.n = g.n; P.b_static = g.b_static;
+    P.n_terms = g.n_terms; P.m = g.m; P.n = g.n; P.b_static = g.b_static;
     for (int t = 0; t < g.n_terms; ++t) {
       const GemmTerm& tm = g.t[t];
       P.kblocks[t] = (tm.k + bk - 1) / bk;
@@ -70,23 +77,17 @@ inline bool fill_group(Group& G, const GemmArgs* gs, int count, const int* order
       P.a_k[t] = tm.a_trans ? 1 : 0;
       P.b_k[t] = tm.b_trans ? 0 : 1;
       P.a_rpad[t] = tm.a_rpad; P.b_rpad[t] = tm.b_rpad; P.k[t] = tm.k;
-      P.b_rows[t] = (int)(tm.b_rows ? tm.b_rows : tm.b_rpad);
       if (!fbl_encode_f32_rtile_map(&P.ta[t], tm.a, tm.a_rpad, (tm.a_trans ? g.m : tm.k) / 32, P.a_k[t] ? bk : bm, (P.a_k[t] ? bm : bk) / 32) ||
           !fbl_encode_f32_rtile_map(&P.tb[t], tm.b, tm.b_rpad, (tm.b_trans ? tm.k : g.n) / 32, P.b_k[t] ? bk : bn, (P.b_k[t] ? bn : bk) / 32, tm.b_rows))
         return false;
     }
     P.tiles_m = (g.m + bm - 1) / bm; P.tiles_n = (g.n + bn - 1) / bn;
     P.c_rpad = g.c_rpad; P.seq = g.seq; P.t_pad = g.t_pad; P.dot_hd = g.dot_hd; P.dot_hq = g.dot_hq;
-    P.areas = g.acc_mode && g.ksplit > 1 ? g.ksplit : 1;
-    P.area_stride = g.c_rpad * g.n;
-    P.dyn = g.dyn;
-    if (g.dyn && (!g.rows || g.n_terms != 1 || g.rows != gs[0].rows)) return false;
   }
   return true;
 }
 inline bool point_group(Group& G, const GemmArgs* gs, int32_t* status) {
   G.status = status;
-  G.rows = gs[0].rows;
   G.zero_ptr = (uint4*)gs[0].zero_ptr; G.zero_vec = (long long)(gs[0].zero_bytes / 16); G.reset_status = gs[0].reset_status;
   bool ok = true;
   for (int i = 0; i < G.count; ++i) {
@@ -98,19 +99,18 @@ inline bool point_group(Group& G, const GemmArgs* gs, int32_t* status) {
     }
     P.c = g.acc_mode ? g.acc : (float*)g.c; P.bias = g.bias; P.residual = g.acc_mode == 2 ? g.acc : (const float*)g.residual;
     P.dot_with = (const float*)g.dot_with; P.dot_out = g.dot_out;
-    P.head = g.head;
   }
   return ok;
 }
 
 using tc::lds4;
 
-// (`area`: where the unit's copy of C begins.)
 // This block's share of the tile's rows: the slices' sums (each block's at `base` of its shared memory, rows LD floats apart)
 // in slice order, bias, residual, padding rows, 16-byte stores.  A thread keeps its four columns and has two rows in flight (one
 // at a time, each waiting for its loads, an 800 x 768 x 768 product took 2 us longer).
-template <int BM, int BN, int LD, int THREADS>
-__device__ __forceinline__ void finish_tile(const Problem& P, int slices, int slice, uint32_t base, int m0, int n0, int64_t area = 0) {
+// HEAD: rows up to m_end are stored, in a copy of C `area` floats on, and the products' rows are not the tokens'.
+template <int BM, int BN, int LD, int THREADS, bool HEAD = false>
+__device__ __forceinline__ void finish_tile(const Problem& P, int slices, int slice, uint32_t base, int m0, int n0, int m_end = 0, int64_t area = 0) {
   constexpr int VECS = BN / 4, STEP = THREADS / VECS, U = 2;
   static_assert(THREADS % VECS == 0, "whole rows");
   const int rows = BM / slices, r0 = slice * rows;
@@ -123,10 +123,10 @@ __device__ __forceinline__ void finish_tile(const Problem& P, int slices, int sl
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int i = i0 + u * STEP, m = m0 + r0 + i;
-      live[u] = i < rows && m < P.m && n < P.n;
+      live[u] = i < rows && m < (HEAD ? m_end : P.m) && n < P.n;
       s[u] = extra[u] = make_float4(0.f, 0.f, 0.f, 0.f);
       if (!live[u]) continue;
-      const int64_t off = area + rt_off<32>(P.c_rpad, m, n);
+      const int64_t off = (HEAD ? area : 0) + rt_off<32>(P.c_rpad, m, n);
       if (P.residual) extra[u] = *reinterpret_cast<const float4*>(P.residual + off);
       else if (P.dot_with) extra[u] = *reinterpret_cast<const float4*>(P.dot_with + off);
     }
@@ -154,9 +154,9 @@ __device__ __forceinline__ void finish_tile(const Problem& P, int slices, int sl
       if (live[u]) {
         float4 v = s[u];
         v.x += bias.x; v.y += bias.y; v.z += bias.z; v.w += bias.w;
-        const int64_t off = area + rt_off<32>(P.c_rpad, m, n);
+        const int64_t off = (HEAD ? area : 0) + rt_off<32>(P.c_rpad, m, n);
         if (P.residual) { v.x += extra[u].x; v.y += extra[u].y; v.z += extra[u].z; v.w += extra[u].w; }
-        if (P.t_pad > 0 && !P.dyn && m % P.t_pad >= P.seq) v = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (!HEAD && P.t_pad > 0 && m % P.t_pad >= P.seq) v = make_float4(0.f, 0.f, 0.f, 0.f);
         *reinterpret_cast<float4*>(P.c + off) = v;
         if (P.dot_with) {
           const float4 q = P.residual ? *reinterpret_cast<const float4*>(P.dot_with + off) : extra[u];

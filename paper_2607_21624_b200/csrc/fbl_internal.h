@@ -107,7 +107,7 @@ struct HeadEpi {
   const int32_t* n;             // how many rows have a loss, which may be none (GemmArgs.rows: at least 1)
   const float* y;
   long long rows;               // pitch of every per-row array here
-  int vocab, col0;              // columns of the vocabulary, and the first one of this product's
+  int vocab, col0, top_k;       // columns of the vocabulary, the first one of this product's, entries a row has at most
   float scale;                  // from a product to a logit times log2 e
   float2* part;                 // forward: [row][column tile, `tiles` of them] (k, sum of 2^((product - k) scale))
   int tiles;
@@ -190,8 +190,11 @@ static inline bool rope_in_projection(const fbl_plan* p, GemmArgs* gs, const flo
 __host__ __device__ __forceinline__ int gemm_slice_begin(int total, int slices, int slice) { return total * slice / slices; }
 struct GemmShape { int64_t m; int n; int kblocks; int splittable; };
 int gemm_tc_choose_split(int sm_count, const GemmShape* sh, int count, bool zero_rides);
+// The head's products: one with an epilogue of the vocabulary's softmax, or dX and dW, or one of them.
+cudaError_t launch_gemm_tc_head(const fbl_plan* p, const GemmArgs* gs, int count, int32_t* status, cudaStream_t st);
 // The same for slices with areas of their own, of dX beside dW (which may be null).
 int gemm_tc_choose_own_slices(int sm_count, const GemmShape* dw, const GemmShape& dx);
+cudaError_t launch_gemm_tc_f32_head(const fbl_plan* p, const GemmArgs* gs, int count, int32_t* status, cudaStream_t st);
 // Areas of an fp32 group's last problem, whose other fields but addresses are set.
 int gemm_tc_f32_choose_areas(const fbl_plan* p, GemmArgs* gs, int count);
 constexpr int HEAD_TILE = 256, HEAD_TILE_F32 = 64;      // columns of a partial of the softmax statistics

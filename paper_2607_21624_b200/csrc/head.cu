@@ -92,7 +92,7 @@ HeadRows rows_of(const fbl_head_plan* p, const void* saved) {
 HeadEpi epilogue_of(const fbl_head_plan* p, const HeadRows& R, int col0) {
   HeadEpi h = {};
   h.ids = R.ids; h.count = R.count; h.row_of = R.row_of; h.n = R.n; h.y = R.y; h.rows = R.rows;
-  h.vocab = p->d.vocab; h.col0 = col0; h.scale = p->scale;
+  h.vocab = p->d.vocab; h.col0 = col0; h.top_k = p->top_k; h.scale = p->scale;
   h.k = R.k; h.sum = R.sum;
   h.inv_tau = 1.f / p->d.temperature;
   return h;
@@ -144,9 +144,9 @@ GemmArgs logits_product(const fbl_head_plan* p, const HeadRows& R, const void* W
 }
 
 int run_products(const fbl_head_plan* p, GemmArgs* gs, int count, int32_t* status, cudaStream_t st) {
-  int k = 0;
-  HEAD_CUDA(run_gemm_group(p->base, gs, count, status, st, -1, &k));
-  p->launches += k;
+  if (p->d.dtype == FBL_DTYPE_FP32) HEAD_CUDA(launch_gemm_tc_f32_head(p->base, gs, count, status, st));
+  else HEAD_CUDA(launch_gemm_tc_head(p->base, gs, count, status, st));
+  p->launches++;
   return FBL_OK;
 }
 #define HEAD_RUN(expr) do { const int rc__ = (expr); if (rc__ != FBL_OK) return rc__; } while (0)
@@ -177,7 +177,7 @@ int fbl_head_plan_create(const fbl_head_desc* desc, fbl_head_plan** out) {
   *out = nullptr;
   const fbl_head_desc& d = *desc;
   if (d.vocab <= 0 || d.top_k < 0 || (d.vocab_rows != 0 && d.vocab_rows != 1)) return FBL_ERR_INVALID_ARG;
-  if (!(d.temperature > 0.f) || isinf(d.temperature)) return FBL_ERR_INVALID_ARG;
+  if (!(d.temperature > 0.f) || isinf(d.temperature) || isinf(1.5f / d.temperature)) return FBL_ERR_INVALID_ARG;
   if (d.top_k == 0 && d.temperature != 1.f) return FBL_ERR_INVALID_ARG;
   if (d.vocab > 1 << 20 || d.top_k > HEAD_MAX_TOP) return FBL_ERR_UNSUPPORTED_SHAPE;
   if (d.batch <= 0 || d.seq <= 0) return FBL_ERR_INVALID_ARG;

@@ -73,8 +73,9 @@ struct Row {
   __device__ __forceinline__ Row() : row(0), count(0), live(false), g(0.f), gs(0.f), k(0.f) {}
   __device__ __forceinline__ Row(const HeadEpi& H, int m, int col, int seq, int t_pad) : g(0.f), gs(0.f), k(0.f) {
     live = m < __ldcg(H.n);
-    row = live ? H.row_of[m] : 0;
-    count = live ? H.count[row] : 0;
+    // (bounded by what the buffers were made for: both lie in the caller's memory)
+    row = live ? (int)min((uint32_t)H.row_of[m], (uint32_t)H.rows - 1u) : 0;
+    count = live ? min(H.count[row], H.top_k) : 0;
     e = Entries(H, row, count, col);
     if (GRAD && count > 0) {
       const int b = row / t_pad, t = row - b * t_pad;
@@ -146,11 +147,10 @@ __device__ __forceinline__ void grad64(const HeadEpi& H, Row<true>& R, uint32_t 
 
 }  // namespace headepi
 
-template <int BN, typename Problem, typename Acc, typename Wait>
-__device__ __forceinline__ bool head_stats_tile(const Problem& P, int m0, int n0, int q, Acc acc, Wait wait) {
-  const HeadEpi& H = P.head;
+template <int BN, typename Acc, typename Wait>
+__device__ __forceinline__ bool head_stats_tile(const HeadEpi& H, int seq, int t_pad, int m0, int n0, int q, Acc acc, Wait wait) {
   const int m = m0 + q * 32 + threadIdx.x % 32;
-  headepi::Row<false> R(H, m, n0, P.seq, P.t_pad);
+  headepi::Row<false> R(H, m, n0, seq, t_pad);
   if (!wait()) return false;
   tc::tc_fence_after();
   float k = -INFINITY, s = 0.f;
@@ -165,8 +165,7 @@ __device__ __forceinline__ bool head_stats_tile(const Problem& P, int m0, int n0
 }
 
 template <int BN, typename Problem, typename Acc, typename Wait>
-__device__ __forceinline__ bool head_grad_tile(const Problem& P, int m0, int n0, int q, Acc acc, uint32_t stg0, int& pc, Wait wait) {
-  const HeadEpi& H = P.head;
+__device__ __forceinline__ bool head_grad_tile(const HeadEpi& H, const Problem& P, int m0, int n0, int q, Acc acc, uint32_t stg0, int& pc, Wait wait) {
   const int lane = threadIdx.x % 32;
   headepi::Row<true> R(H, m0 + q * 32 + lane, H.col0 + n0, P.seq, P.t_pad);
   if (!wait()) return false;

@@ -228,8 +228,6 @@ bool gemm_ffma_supported(const fbl_plan* p, const GemmArgs& g) {
 static cudaError_t make_group(FfmaLaunch& L, const fbl_plan* p, const GemmArgs* gs, int count) {
   FfmaGroup& G = L.G;
   const int order[f32g::MAX_PROBLEMS] = {0, 1, 2, 3, 4};
-  for (int i = 0; i < count; ++i)
-    if (gs[i].dyn || gs[i].acc_mode) return cudaErrorInvalidValue;              // not on this path
   if (!f32g::fill_group(G, gs, count, order, BM, BN, BK)) return cudaErrorInvalidValue;
   int tiles = 0;
   for (int i = 0; i < count; ++i) tiles += G.p[i].tiles_m * G.p[i].tiles_n;

@@ -352,7 +352,7 @@ __global__ void __launch_bounds__(256) head_scatter_kernel(const float* __restri
     const int64_t line = i / TW, panel = line / R.rows;
     const int pos = R.pos[line - panel * R.rows];
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (pos >= 0) {
+    if (pos >= 0 && pos < R.rows) {
       const float* from = acc + (panel * R.rows + pos) * TW + i % TW;
 #pragma unroll 8
       for (int k = group; k < areas; k += GROUPS) {

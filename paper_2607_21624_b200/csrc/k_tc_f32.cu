@@ -63,7 +63,7 @@ using tc::sts4;
 // is not finite, which an infinity makes of every product that it is in.  32 columns of the reduction at a time, at `stage` in shared memory as
 // [column][row]; a thread has four rows and BN / 16 columns of the tile, which goes to `tile` (rows LD floats apart).
 template <int BN>
-__device__ __noinline__ void plain_tile(const Problem& P, uint32_t tile, uint32_t stage, int m0, int n0, int kb_begin, int kb_end) {
+__device__ __noinline__ void plain_tile(const Problem& P, uint32_t tile, uint32_t stage, int m0, int n0, int kb_begin, int kb_end, int m_end, int b_rows) {
   constexpr int KS = 32, LDA = BM + 4, LDB = BN + 4, NV = BN / 64, GROUPS = 512;
   static_assert(KS * (LDA + LDB) * 4 <= (int)(6 * Smem<BN>::PART) && GROUPS <= THREADS && GROUPS * 4 * 4 * NV == BM * BN, "parts' area, a thread's results");
   const uint32_t sa = stage, sb = stage + KS * LDA * 4;
@@ -98,8 +98,8 @@ __device__ __noinline__ void plain_tile(const Problem& P, uint32_t tile, uint32_
 #pragma unroll 1
     for (int k0 = kb * BK; k0 < min(kb * BK + BK, P.k[t]); k0 += KS) {
       __syncthreads();
-      fill(sa, LDA, BM, P.a[t], P.a_rpad[t], P.a_k[t] != 0, m0, P.m, k0, P.k[t]);
-      fill(sb, LDB, BN, P.b[t], P.b_rpad[t], P.b_k[t] != 0, n0, P.b_k[t] ? P.n : min(P.n, P.b_rows[t]), k0, P.b_k[t] ? min(P.k[t], P.b_rows[t]) : P.k[t]);
+      fill(sa, LDA, BM, P.a[t], P.a_rpad[t], P.a_k[t] != 0, m0, m_end, k0, P.k[t]);
+      fill(sb, LDB, BN, P.b[t], P.b_rpad[t], P.b_k[t] != 0, n0, P.b_k[t] ? P.n : min(P.n, b_rows), k0, P.b_k[t] ? min(P.k[t], b_rows) : P.k[t]);
       __syncthreads();
       if (threadIdx.x < GROUPS) {
 #pragma unroll 4
@@ -127,10 +127,13 @@ __device__ __noinline__ void plain_tile(const Problem& P, uint32_t tile, uint32_
   __syncthreads();
 }
 
-// EPI: what a tile's sums become.  The head's epilogues take whole sums: one slice.
-enum { F32_PLAIN = 0, F32_HEAD_STATS, F32_HEAD_GRAD };
+// EPI: what a tile's sums become.  The head's: statistics or gradients of the vocabulary's softmax, of whole sums (one slice), and dX and dW.
+enum { F32_LAYER = 0, F32_HEAD_STATS, F32_HEAD_GRAD, F32_HEAD_OUT };
+template <int EPI> struct GroupKind { using type = f32g::HeadGroup; };
+template <> struct GroupKind<F32_LAYER> { using type = Group; };
 template <int BN, int EPI>
-__global__ void __launch_bounds__(THREADS, 1) gemm_tc_f32_kernel(const __grid_constant__ Group G) {
+__global__ void __launch_bounds__(THREADS, 1) gemm_tc_f32_kernel(const __grid_constant__ typename GroupKind<EPI>::type G) {
+  constexpr bool HEAD = EPI != F32_LAYER, SOFTMAX = EPI == F32_HEAD_STATS || EPI == F32_HEAD_GRAD;
   using SM = Smem<BN>;
   constexpr int STAGES = SM::STAGES;
   extern __shared__ uint8_t smem_raw[];
@@ -144,19 +147,22 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_tc_f32_kernel(const __grid_co
   const int warp = (int)tc::uniform(threadIdx.x / 32), lane = threadIdx.x % 32;
   const tc::Status status(G.status, G.reset_status);
   // work unit: (problem, tile, area, slice); the slices of a tile are the blocks of a cluster
-  const int slice = blockIdx.x % G.slices;
-  int w = blockIdx.x / G.slices, pi = 0;
-  while (w >= G.p[pi].tiles_m * G.p[pi].tiles_n * G.p[pi].areas) { w -= G.p[pi].tiles_m * G.p[pi].tiles_n * G.p[pi].areas; ++pi; }
-  const Problem& P = G.p[pi];
-  const int area = w % P.areas;
-  w /= P.areas;
-  const int m0 = (w % P.tiles_m) * BM, n0 = (w / P.tiles_m) * BN;
-  int total_kb = P.total_kb;
-  if (P.dyn) {                               // fewer rows, or less to reduce, than the launch was made for
-    pdl_wait();
-    const int rows = __ldcg(G.rows);
-    if (P.dyn == 1 && m0 >= rows) return;      // all blocks of a cluster alike
-    if (P.dyn == 2) total_kb = (rows + BK - 1) / BK;
+  int total_kb = 0, area = 0;
+  auto areas = [&](int i) {
+    if constexpr (HEAD) return G.h[i].areas;
+    else return 1;
+  };
+  if constexpr (HEAD) {                        // fewer rows, or less to reduce, than the launch was made for
+    int w = blockIdx.x / G.slices, pi = 0;
+    while (w >= G.p[pi].tiles_m * G.p[pi].tiles_n * areas(pi)) { w -= G.p[pi].tiles_m * G.p[pi].tiles_n * areas(pi); ++pi; }
+    total_kb = G.p[pi].total_kb;
+    area = w % areas(pi);
+    if (G.h[pi].dyn) {
+      pdl_wait();
+      const int rows = __ldcg(G.rows);
+      if (G.h[pi].dyn == 1 && w / areas(pi) % G.p[pi].tiles_m * BM >= rows) return;      // all blocks of a cluster alike
+      if (G.h[pi].dyn == 2) total_kb = min((max(rows, 1) - 1) / BK + 1, total_kb);
+    }
   }
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) {
@@ -182,11 +188,17 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_tc_f32_kernel(const __grid_co
   asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem_base) : "r"(slot));
   tmem_base = tc::uniform(tmem_base);
   pdl_launch_dependents();
-  const int area_kb = gemm_slice_begin(total_kb, P.areas, area), area_n = gemm_slice_begin(total_kb, P.areas, area + 1) - area_kb;
+  const int slice = blockIdx.x % G.slices;
+  int w = blockIdx.x / G.slices, pi = 0;
+  while (w >= G.p[pi].tiles_m * G.p[pi].tiles_n * areas(pi)) { w -= G.p[pi].tiles_m * G.p[pi].tiles_n * areas(pi); ++pi; }
+  const Problem& P = G.p[pi];
+  w /= areas(pi);
+  const int m0 = (w % P.tiles_m) * BM, n0 = (w / P.tiles_m) * BN;
+  if constexpr (!HEAD) total_kb = P.total_kb;
+  const int area_kb = HEAD ? gemm_slice_begin(total_kb, areas(pi), area) : 0, area_n = HEAD ? gemm_slice_begin(total_kb, areas(pi), area + 1) - area_kb : total_kb;
   const int kb_begin = area_kb + gemm_slice_begin(area_n, G.slices, slice), n_kb = area_kb + gemm_slice_begin(area_n, G.slices, slice + 1) - kb_begin;
-
-  // the head: a lane of the last eight warps has half a row of the tile, 64 columns
-  static_assert(EPI == F32_PLAIN || BN == 128, "half a row is 64 columns");
+  // a lane of the last eight warps has half a row of the tile, 64 columns
+  static_assert(!SOFTMAX || BN == 128, "half a row is 64 columns");
   headepi::Row<EPI == F32_HEAD_GRAD> R;
   const int half_m = m0 + warp % 4 * 32 + lane, half_n = n0 + (warp - 10) / 4 * 64;
   if (warp == 0) {
@@ -314,7 +326,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_tc_f32_kernel(const __grid_co
     for (int i = 0; i < N / 2; ++i) sum[i] = make_float2(0.f, 0.f);
     pdl_wait();
     f32g::group_chores(G, threadIdx.x - 10 * 32, 256);
-    if constexpr (EPI != F32_PLAIN) R = headepi::Row<EPI == F32_HEAD_GRAD>(P.head, half_m, P.head.col0 + half_n, P.seq, P.t_pad);
+    if constexpr (SOFTMAX) R = headepi::Row<EPI == F32_HEAD_GRAD>(G.epi, half_m, G.epi.col0 + half_n, P.seq, P.t_pad);
     for (int it = 0; it < n_kb; ++it) {
       const int b = it & 1;
       if (!tc::mbar_wait(done(b), (it >> 1) & 1, status, 138)) break;
@@ -348,10 +360,13 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_tc_f32_kernel(const __grid_co
   __syncthreads();
   uint32_t again;
   asm volatile("ld.shared.u32 %0, [%1];" : "=r"(again) : "r"(flag) : "memory");
-  if (again) plain_tile<BN>(P, base, base + SM::PARTS_OFF, m0, n0, kb_begin, kb_begin + n_kb);
+  if (again) {
+    if constexpr (HEAD) plain_tile<BN>(P, base, base + SM::PARTS_OFF, m0, n0, kb_begin, kb_begin + n_kb, G.h[pi].m_stored, G.h[pi].b_rows);
+    else plain_tile<BN>(P, base, base + SM::PARTS_OFF, m0, n0, kb_begin, kb_begin + n_kb, P.m, 0x7fffffff);
+  }
   if (G.slices > 1) tc::cluster_sync_all();
   if (warp == 1) tc::tmem_dealloc(tmem_base, TMEM_COLS);
-  if constexpr (EPI != F32_PLAIN) {
+  if constexpr (SOFTMAX) {
     if (warp >= 10 && half_n < P.n) {
       const uint32_t at = base + (uint32_t)((warp % 4 * 32 + lane) * SM::LD + (half_n - n0)) * 4;
       uint32_t v[64];
@@ -359,10 +374,10 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_tc_f32_kernel(const __grid_co
       for (int j = 0; j < 64; j += 4) *reinterpret_cast<float4*>(&v[j]) = lds4(at + j * 4);
       if constexpr (EPI == F32_HEAD_STATS) {
         float k = -INFINITY, s = 0.f;
-        headepi::stats64(P.head, R, v, half_n, k, s);
-        if (R.live) P.head.part[(long long)R.row * P.head.tiles + half_n / HEAD_TILE_F32] = make_float2(k, s);
+        headepi::stats64(G.epi, R, v, half_n, k, s);
+        if (R.live) G.epi.part[(long long)R.row * G.epi.tiles + half_n / HEAD_TILE_F32] = make_float2(k, s);
       } else {
-        headepi::grad64(P.head, R, v, P.head.col0 + half_n);
+        headepi::grad64(G.epi, R, v, G.epi.col0 + half_n);
 #pragma unroll
         for (int j = 0; j < 64; ++j) v[j] = R.count ? v[j] : 0u;
 #pragma unroll
@@ -372,11 +387,12 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_tc_f32_kernel(const __grid_co
     if (EPI == F32_HEAD_STATS) return;
     __syncthreads();
   }
-  f32g::finish_tile<BM, BN, SM::LD, THREADS>(P, G.slices, slice, base, m0, n0, area * P.area_stride);
+  if constexpr (HEAD) f32g::finish_tile<BM, BN, SM::LD, THREADS, true>(P, G.slices, slice, base, m0, n0, G.h[pi].m_stored, area * G.h[pi].area_stride);
+  else f32g::finish_tile<BM, BN, SM::LD, THREADS>(P, G.slices, slice, base, m0, n0);
   if (G.slices > 1) tc::cluster_sync_all();      // no block leaves while another may still read its partial tile
 }
 
-struct Launch { Group G; int grid, bn; void (*kernel)(const Group); };
+struct Launch { Group G; int grid, bn; };
 
 // Tile width (128, 64) and slices (1, 2, 4, 8: blocks of a cluster) of a launch: the shortest list schedule, in the order of the
 // grid, of its tiles over the clusters that fit the part at once.  Measured: a block takes some 6 us (64 columns: 4.5) to come up,
@@ -436,7 +452,6 @@ Choice choose(const fbl_plan* p, const GemmArgs* gs, const int* order, int count
 
 cudaError_t launch_gemm_tc_f32_group(const fbl_plan* p, const GemmArgs* gs, int count, int32_t* status, cudaStream_t st) {
   if (count < 1 || count > f32g::MAX_PROBLEMS) return cudaErrorInvalidValue;
-  if (gs[0].epi >= 6 && (count != 1 || !gs[0].head.n || gs[0].acc_mode || gs[0].residual || gs[0].bias)) return cudaErrorInvalidValue;
   LaunchKey key;
   gemm_group_key(key, gs, count);
   return LaunchMemo<Launch, 12>::run(p, FBL_MEMO_TC_F32_GEMM, key,
@@ -446,18 +461,65 @@ cudaError_t launch_gemm_tc_f32_group(const fbl_plan* p, const GemmArgs* gs, int 
         const Choice c = choose(p, gs, order, count);
         if (!f32g::fill_group(L.G, gs, count, order, BM, c.bn, BK)) return cudaErrorInvalidValue;
         L.grid = 0;
-        for (int i = 0; i < count; ++i) L.grid += L.G.p[i].tiles_m * L.G.p[i].tiles_n * L.G.p[i].areas * c.slices;
+        for (int i = 0; i < count; ++i) L.grid += L.G.p[i].tiles_m * L.G.p[i].tiles_n * c.slices;
         L.G.slices = c.slices;
         L.bn = c.bn;
-        L.kernel = gs[0].epi == 6 ? gemm_tc_f32_kernel<128, F32_HEAD_STATS> : gs[0].epi == 7 ? gemm_tc_f32_kernel<128, F32_HEAD_GRAD>
-                   : c.bn == 128 ? gemm_tc_f32_kernel<128, F32_PLAIN> : gemm_tc_f32_kernel<64, F32_PLAIN>;
-        return cudaFuncSetAttribute(L.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(c.bn == 128 ? Smem<128>::TOTAL : Smem<64>::TOTAL));
+        const cudaError_t e = cudaFuncSetAttribute(gemm_tc_f32_kernel<128, F32_LAYER>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Smem<128>::TOTAL);
+        return e != cudaSuccess ? e : cudaFuncSetAttribute(gemm_tc_f32_kernel<64, F32_LAYER>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Smem<64>::TOTAL);
       },
       [&](Launch& L) { return f32g::point_group(L.G, gs, status); },
       [&](const Launch& L) {
-        const size_t smem = L.bn == 128 ? Smem<128>::TOTAL : Smem<64>::TOTAL;
-        if (L.G.slices > 1) return launch_cluster(L.kernel, dim3(L.grid), dim3(THREADS), smem, st, L.G.slices, true, L.G);
-        return launch_pdl(L.kernel, dim3(L.grid), dim3(THREADS), smem, st, L.G);
+        auto go = [&](auto kernel, size_t smem) {
+          if (L.G.slices > 1) return launch_cluster(kernel, dim3(L.grid), dim3(THREADS), smem, st, L.G.slices, true, L.G);
+          return launch_pdl(kernel, dim3(L.grid), dim3(THREADS), smem, st, L.G);
+        };
+        return L.bn == 128 ? go(gemm_tc_f32_kernel<128, F32_LAYER>, Smem<128>::TOTAL) : go(gemm_tc_f32_kernel<64, F32_LAYER>, Smem<64>::TOTAL);
+      });
+}
+
+namespace {
+struct HeadLaunch { f32g::HeadGroup G; int grid; size_t smem; void (*kernel)(const f32g::HeadGroup); };
+}  // namespace
+
+cudaError_t launch_gemm_tc_f32_head(const fbl_plan* p, const GemmArgs* gs, int count, int32_t* status, cudaStream_t st) {
+  if (count < 1 || count > 2 || (gs[0].epi && (count != 1 || gs[0].epi < 6 || gs[0].epi > 7))) return cudaErrorInvalidValue;
+  for (int i = 0; i < count; ++i)
+    if (!gs[i].rows || gs[i].rows != gs[0].rows || gs[i].n_terms != 1 || gs[i].bias || gs[i].residual || gs[i].dot_with) return cudaErrorInvalidValue;
+  LaunchKey key;
+  gemm_group_key(key, gs, count);
+  return LaunchMemo<HeadLaunch, 12>::run(p, FBL_MEMO_TC_F32_GEMM, key,
+      [&](HeadLaunch& L) {
+        int order[f32g::MAX_PROBLEMS];
+        f32g::longest_first(gs, count, order);
+        const Choice c = choose(p, gs, order, count);
+        memset(static_cast<void*>(&L.G), 0, sizeof(L.G));
+        if (!f32g::fill_group(L.G, gs, count, order, BM, c.bn, BK)) return cudaErrorInvalidValue;
+        L.grid = 0;
+        for (int i = 0; i < count; ++i) {
+          const GemmArgs& g = gs[order[i]];
+          f32g::HeadProblem& H = L.G.h[i];
+          // with rows enough for one tile at most, there is nothing to leave out
+          H.dyn = g.dyn == 1 && g.m <= BM ? 0 : g.dyn;
+          H.areas = g.acc_mode && g.ksplit > 1 ? g.ksplit : 1;
+          H.area_stride = g.c_rpad * g.n;
+          H.m_stored = g.c_rows ? (int)g.c_rows : g.m;
+          H.b_rows = (int)(g.t[0].b_rows ? g.t[0].b_rows : g.t[0].b_rpad);
+          L.grid += L.G.p[i].tiles_m * L.G.p[i].tiles_n * H.areas * c.slices;
+        }
+        L.G.slices = c.slices;
+        L.smem = c.bn == 128 ? Smem<128>::TOTAL : Smem<64>::TOTAL;
+        L.kernel = gs[0].epi == 6 ? gemm_tc_f32_kernel<128, F32_HEAD_STATS> : gs[0].epi == 7 ? gemm_tc_f32_kernel<128, F32_HEAD_GRAD>
+                   : c.bn == 128 ? gemm_tc_f32_kernel<128, F32_HEAD_OUT> : gemm_tc_f32_kernel<64, F32_HEAD_OUT>;
+        return cudaFuncSetAttribute(L.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)L.smem);
+      },
+      [&](HeadLaunch& L) {
+        L.G.rows = gs[0].rows;
+        L.G.epi = gs[0].head;
+        return f32g::point_group(L.G, gs, status);
+      },
+      [&](const HeadLaunch& L) {
+        if (L.G.slices > 1) return launch_cluster(L.kernel, dim3(L.grid), dim3(THREADS), L.smem, st, L.G.slices, true, L.G);
+        return launch_pdl(L.kernel, dim3(L.grid), dim3(THREADS), L.smem, st, L.G);
       });
 }
 

@@ -41,17 +41,11 @@ struct alignas(64) TcProblem {
   // later kernel rounds the sums to bf16.  Single-term problems without epilogue extras only.
   int ksplit;
   CUtensorMap tacc;
-  int sums, slice_panels;          // sums: 0 rounded to C, 1 stored, 2 added to tacc's buffer; slice_panels: from one slice's area to the next
-  HeadEpi head;
-  int dyn;                         // 1: G.rows rows instead of m, 2: a reduction over G.rows
-  const float* over;               // C = alpha / max(*over, 1) times the product, where not null
-  float alpha;
   // Fused activation of the feed-forward block (kernel variant EPI only; `residual` then points at the first extra
   // operand U instead of a residual, `aux1` at the second one, G; `tc2` is the second output's map):
   //   1 GELU forward    C = v (U), C2 = gelu(v)           2 GELU backward    C = v gelu'(U)
   //   3 gated forward   C = v (G), C2 = silu(v) U          4 gated backward   C = v silu(G), C2 = v U silu'(G)
   //   5 rotary embedding C = v with each 64-column head's (i, i + 32) pairs turned by the table's angle of the row's token
-  //   6, 7 (kernel variants of their own) the vocabulary's softmax, head_epilogue.cuh
   const float2* rope;      // [32][t_pad] cosine and sine
   int epi;
   const __nv_bfloat16* aux1;
@@ -63,17 +57,34 @@ struct alignas(64) TcGroup {
   int late_trigger;                          // as in GemmArgs: the dependents' trigger comes after the wait
   int slices;                                // gemm_tc_split_kernel: blocks of a cluster, which share a tile's reduction
   int32_t* status;
-  const int32_t* rows;                       // see GemmArgs
-  int dynamic;                               // 1: the work list depends on it
-  // Of two problems, the first with longer units than the second: deal them out as Deal does, with a unit's clocks per k-block, and
-  // at least `floor` (its epilogue) beside them (0: in turn)
-  float kb_clocks, unit_clocks, floor_clocks;
   // Optional chores for the epilogue warps while the first tile's main loop runs: zero-fill a buffer that a later
   // kernel of the pass adds into (16-byte units, dealt evenly to the blocks), and reset the pass's status word.
   uint4* zero_ptr;
   long long zero_vec;
   int reset_status;
 };
+
+// What the head's launches have besides (kernel variants of their own, EPI_HEAD_*).
+struct HeadProblem {
+  int dyn;                                   // 1: rows counted by `rows` instead of m, 2: a reduction over them
+  int sums, slice_panels;                    // 1: fp32 sums stored, 2: added, in an area a slice; 0: rounded to C
+  const float* over;                         // C = alpha / max(*over, 1) times the product, where not null
+  float alpha;
+};
+struct alignas(64) TcHeadGroup : TcGroup {
+  HeadProblem h[2];
+  HeadEpi epi;
+  const int32_t* rows;                       // see GemmArgs
+  int dynamic;                               // 1: the work list depends on it
+  // Of two problems, the first with longer units than the second: deal them out as Deal does, with a unit's clocks per k-block, and
+  // at least `floor` (its epilogue) beside them (0: in turn)
+  float kb_clocks, unit_clocks, floor_clocks;
+};
+enum { EPI_NONE = 0, EPI_ACT, EPI_ROPE, EPI_HEAD_STATS, EPI_HEAD_GRAD, EPI_HEAD_OUT };
+template <int EPI> constexpr bool IS_HEAD = EPI >= EPI_HEAD_STATS;
+template <bool HEAD> struct GroupKind { using type = TcGroup; };
+template <> struct GroupKind<true> { using type = TcHeadGroup; };
+template <int EPI> using GroupOf = typename GroupKind<IS_HEAD<EPI>>::type;
 
 __device__ __forceinline__ void group_chores(const TcGroup& G, int tid, int n_threads) {
   if (G.reset_status && blockIdx.x == 0 && tid == 0) *G.status = G.status[FBL_EARLY_COLSUM] = G.status[FBL_EARLY_ROUND] = 0;
@@ -106,18 +117,66 @@ struct SmemPlan {
 // fastest (blocks that run together then share the B tiles of one weight column block through L2).
 struct TileCoord { int prob, m0, n0, kb0, kb1, slice; };     // kb0..kb1: k-block range of term 0 (split problems)
 
-// `rows`: the device's number of rows, for problems that go by it.
-__device__ __forceinline__ int rows_of(const TcProblem& P, int rows) { return P.dyn == 1 ? rows : P.m; }
-__device__ __forceinline__ int kblocks_of(const TcProblem& P, int rows) { return P.dyn == 2 ? (rows + BK - 1) / BK : P.kblocks[0]; }
-// Before a role's first look at the work list.
-__device__ __forceinline__ int dynamic_rows(const TcGroup& G) {
-  if (!G.dynamic) return 0;
-  pdl_wait();
-  return __ldcg(G.rows);
+template <int BN>
+__device__ __forceinline__ bool tile_at(const TcGroup& G, int w, TileCoord* tc_out) {
+  for (int p = 0; p < G.count; ++p) {
+    const TcProblem& P = G.p[p];
+    const int tm = (P.m + BM - 1) / BM, tn = (P.n + BN - 1) / BN;
+    const int units = tm * tn * P.ksplit;
+    if (w < units) {
+      const int slice = w % P.ksplit, t = w / P.ksplit;        // slices of one tile are neighbours in the list
+      tc_out->prob = p;
+      tc_out->m0 = (t % tm) * BM;
+      tc_out->n0 = (t / tm) * BN;
+      const int per = (P.kblocks[0] + P.ksplit - 1) / P.ksplit;
+      tc_out->kb0 = slice * per;
+      tc_out->kb1 = min(P.kblocks[0], (slice + 1) * per);
+      return true;
+    }
+    w -= units;
+  }
+  return false;
 }
 
-__device__ __forceinline__ void coord(const TcProblem& P, int rows, int p, int slice, int m0, int n0, TileCoord* tc_out) {
-  const int kb = kblocks_of(P, rows), per = (kb + P.ksplit - 1) / P.ksplit;
+// work list in 256 x 256 tiles (ksplit slices as in tile_at); m0 / n0 are the pair's.  Tall problems go in bands of eight row
+// tiles: the 74 tiles at work then share eight row tiles and nine column tiles of operands instead of 32 and two or three, which
+// L2 holds (8192 x 4096 attention step: 5060 -> 4945 us, its four product launches 535, 172, 378, 1191 -> 505, 167, 364, 1131; bands
+// of 16 the same).  Up to 16 row tiles fit as they are (4096 x 2048 x 8192 feed-forward in bands of eight: 88 -> 92 us a launch).
+constexpr int PAIR_BAND = 8, PAIR_BAND_FROM = 16;
+__device__ __forceinline__ bool pair_tile_at(const TcGroup& G, int w, TileCoord* tc_out) {
+  for (int p = 0; p < G.count; ++p) {
+    const TcProblem& P = G.p[p];
+    const int tm = (P.m + 255) / 256, tn = (P.n + 255) / 256;
+    const int units = tm * tn * P.ksplit;
+    if (w < units) {
+      const int slice = w % P.ksplit, t = w / P.ksplit;
+      tc_out->prob = p;
+      const int band = tm > PAIR_BAND_FROM ? PAIR_BAND : tm, at = t / (band * tn), h = min(band, tm - at * band), u = t - at * band * tn;
+      tc_out->m0 = (at * band + u % h) * 256;
+      tc_out->n0 = (u / h) * 256;
+      const int per = (P.kblocks[0] + P.ksplit - 1) / P.ksplit;
+      tc_out->kb0 = slice * per;
+      tc_out->kb1 = min(P.kblocks[0], (slice + 1) * per);
+      return true;
+    }
+    w -= units;
+  }
+  return false;
+}
+
+// `rows`: the device's number of rows, for problems that go by it.  (Bounded by what the launch was made for: the number lies in the
+// caller's memory.)
+__device__ __forceinline__ int rows_of(const TcProblem& P, const HeadProblem& H, int rows) { return H.dyn == 1 ? min(rows, P.m) : P.m; }
+__device__ __forceinline__ int kblocks_of(const TcProblem& P, const HeadProblem& H, int rows) { return H.dyn == 2 ? min((rows + BK - 1) / BK, P.kblocks[0]) : P.kblocks[0]; }
+// Before a role's first look at the work list.
+__device__ __forceinline__ int dynamic_rows(const TcHeadGroup& G) {
+  if (!G.dynamic) return 0;
+  pdl_wait();
+  return min(max(__ldcg(G.rows), 1), 1 << 30);
+}
+
+__device__ __forceinline__ void coord(const TcProblem& P, const HeadProblem& H, int rows, int p, int slice, int m0, int n0, TileCoord* tc_out) {
+  const int kb = kblocks_of(P, H, rows), per = (kb + P.ksplit - 1) / P.ksplit;
   tc_out->prob = p;
   tc_out->m0 = m0;
   tc_out->n0 = n0;
@@ -125,27 +184,23 @@ __device__ __forceinline__ void coord(const TcProblem& P, int rows, int p, int s
   tc_out->kb0 = slice * per;
   tc_out->kb1 = min(kb, (slice + 1) * per);
 }
-// Tiles of a problem: 128 x BN, or a pair's 256 x 256.  Tall problems go in bands of eight row
-// tiles of pairs: the 74 tiles at work then share eight row tiles and nine column tiles of operands instead of 32 and two or three, which
-// L2 holds (8192 x 4096 attention step: 5060 -> 4945 us, its four product launches 535, 172, 378, 1191 -> 505, 167, 364, 1131; bands
-// of 16 the same).  Up to 16 row tiles fit as they are (4096 x 2048 x 8192 feed-forward in bands of eight: 88 -> 92 us a launch).
-constexpr int PAIR_BAND = 8, PAIR_BAND_FROM = 16;
+// Tiles of a problem: 128 x BN, or a pair's 256 x 256 in bands as pair_tile_at has them.
 template <int BN>
 struct OneBlock {
-  static __device__ __forceinline__ int tm(const TcProblem& P, int rows) { return (rows_of(P, rows) + BM - 1) / BM; }
-  static __device__ __forceinline__ int units(const TcProblem& P, int rows) { return tm(P, rows) * ((P.n + BN - 1) / BN) * P.ksplit; }
-  static __device__ __forceinline__ void at(const TcProblem& P, int rows, int p, int w, TileCoord* tc_out) {
-    const int m = tm(P, rows), slice = w % P.ksplit, t = w / P.ksplit;        // slices of one tile are neighbours in the list
-    coord(P, rows, p, slice, (t % m) * BM, (t / m) * BN, tc_out);
+  static __device__ __forceinline__ int tm(const TcProblem& P, const HeadProblem& H, int rows) { return (rows_of(P, H, rows) + BM - 1) / BM; }
+  static __device__ __forceinline__ int units(const TcProblem& P, const HeadProblem& H, int rows) { return tm(P, H, rows) * ((P.n + BN - 1) / BN) * P.ksplit; }
+  static __device__ __forceinline__ void at(const TcProblem& P, const HeadProblem& H, int rows, int p, int w, TileCoord* tc_out) {
+    const int m = tm(P, H, rows), slice = w % P.ksplit, t = w / P.ksplit;        // slices of one tile are neighbours in the list
+    coord(P, H, rows, p, slice, (t % m) * BM, (t / m) * BN, tc_out);
   }
 };
 struct BlockPair {
-  static __device__ __forceinline__ int tm(const TcProblem& P, int rows) { return (rows_of(P, rows) + 255) / 256; }
-  static __device__ __forceinline__ int units(const TcProblem& P, int rows) { return tm(P, rows) * ((P.n + 255) / 256) * P.ksplit; }
-  static __device__ __forceinline__ void at(const TcProblem& P, int rows, int p, int w, TileCoord* tc_out) {
-    const int m = tm(P, rows), tn = (P.n + 255) / 256, slice = w % P.ksplit, t = w / P.ksplit;
+  static __device__ __forceinline__ int tm(const TcProblem& P, const HeadProblem& H, int rows) { return (rows_of(P, H, rows) + 255) / 256; }
+  static __device__ __forceinline__ int units(const TcProblem& P, const HeadProblem& H, int rows) { return tm(P, H, rows) * ((P.n + 255) / 256) * P.ksplit; }
+  static __device__ __forceinline__ void at(const TcProblem& P, const HeadProblem& H, int rows, int p, int w, TileCoord* tc_out) {
+    const int m = tm(P, H, rows), tn = (P.n + 255) / 256, slice = w % P.ksplit, t = w / P.ksplit;
     const int band = m > PAIR_BAND_FROM ? PAIR_BAND : m, at = t / (band * tn), h = min(band, m - at * band), u = t - at * band * tn;
-    coord(P, rows, p, slice, (at * band + u % h) * 256, (u / h) * 256, tc_out);
+    coord(P, H, rows, p, slice, (at * band + u % h) * 256, (u / h) * 256, tc_out);
   }
 };
 
@@ -158,12 +213,12 @@ struct Deal {
   int slot, slots, rows;
   int longs, shorts, light, head, base;      // this block's units; blocks that go first; short units that they get first, and all of those
   bool balanced;
-  __device__ __forceinline__ Deal(const TcGroup& G, int slot_, int slots_, int rows_) : slot(slot_), slots(slots_), rows(rows_), balanced(G.kb_clocks > 0.f) {
+  __device__ __forceinline__ Deal(const TcHeadGroup& G, int slot_, int slots_, int rows_) : slot(slot_), slots(slots_), rows(rows_), balanced(G.kb_clocks > 0.f) {
     if (!balanced) return;
     const TcProblem &A = G.p[0], &B = G.p[1];
-    const int u = Tiles::units(A, rows), v = Tiles::units(B, rows), over = u % slots;
-    const int kb = kblocks_of(A, rows), per = (kb + A.ksplit - 1) / A.ksplit;
-    const float a = fmaxf(per * G.kb_clocks + G.unit_clocks, G.floor_clocks), b = fmaxf(kblocks_of(B, rows) * G.kb_clocks + G.unit_clocks, G.floor_clocks);
+    const int u = Tiles::units(A, G.h[0], rows), v = Tiles::units(B, G.h[1], rows), over = u % slots;
+    const int kb = kblocks_of(A, G.h[0], rows), per = (kb + A.ksplit - 1) / A.ksplit;
+    const float a = fmaxf(per * G.kb_clocks + G.unit_clocks, G.floor_clocks), b = fmaxf(kblocks_of(B, G.h[1], rows) * G.kb_clocks + G.unit_clocks, G.floor_clocks);
     light = slots - over;
     head = over ? min((int)(a / b + 0.5f), v / light) : 0;
     base = light * head;
@@ -171,31 +226,63 @@ struct Deal {
     const int rest = v - base - slot;
     shorts = (slot < over ? 0 : head) + (rest > 0 ? (rest + slots - 1) / slots : 0);
   }
-  __device__ __forceinline__ bool at(const TcGroup& G, int k, TileCoord* tc_out) const {
+  __device__ __forceinline__ bool at(const TcHeadGroup& G, int k, TileCoord* tc_out) const {
     if (balanced) {
       if (k >= longs + shorts) return false;
       const bool odd = slot & 1;
       if (odd ? k >= shorts : k < longs) {
-        Tiles::at(G.p[0], rows, 0, slot + (odd ? k - shorts : k) * slots, tc_out);
+        Tiles::at(G.p[0], G.h[0], rows, 0, slot + (odd ? k - shorts : k) * slots, tc_out);
         return true;
       }
       int j = odd ? k : k - longs;
       const int over = slots - light;
       if (slot >= over) {
-        if (j < head) { Tiles::at(G.p[1], rows, 1, slot - over + j * light, tc_out); return true; }
+        if (j < head) { Tiles::at(G.p[1], G.h[1], rows, 1, slot - over + j * light, tc_out); return true; }
         j -= head;
       }
-      Tiles::at(G.p[1], rows, 1, base + slot + j * slots, tc_out);
+      Tiles::at(G.p[1], G.h[1], rows, 1, base + slot + j * slots, tc_out);
       return true;
     }
     int w = slot + k * slots;
     for (int p = 0; p < G.count; ++p) {
-      const int units = Tiles::units(G.p[p], rows);
-      if (w < units) { Tiles::at(G.p[p], rows, p, w, tc_out); return true; }
+      const int units = Tiles::units(G.p[p], G.h[p], rows);
+      if (w < units) { Tiles::at(G.p[p], G.h[p], rows, p, w, tc_out); return true; }
       w -= units;
     }
     return false;
   }
+};
+
+// A role's way through its block's work list: in turn for the layers' launches, as Deal has it for the head's.
+template <int BN, bool HEAD>
+struct Walk {
+  int w;
+  __device__ __forceinline__ explicit Walk(const TcGroup&) : w(blockIdx.x) {}
+  __device__ __forceinline__ bool at(const TcGroup& G, TileCoord* tcd) const { return tile_at<BN>(G, w, tcd); }
+  __device__ __forceinline__ void step() { w += gridDim.x; }
+};
+template <int BN>
+struct Walk<BN, true> {
+  Deal<OneBlock<BN>> deal;
+  int k;
+  __device__ __forceinline__ explicit Walk(const TcHeadGroup& G) : deal(G, blockIdx.x, gridDim.x, dynamic_rows(G)), k(0) {}
+  __device__ __forceinline__ bool at(const TcHeadGroup& G, TileCoord* tcd) const { return deal.at(G, k, tcd); }
+  __device__ __forceinline__ void step() { ++k; }
+};
+template <bool HEAD>
+struct PairWalk {
+  int w;
+  __device__ __forceinline__ explicit PairWalk(const TcGroup&) : w(blockIdx.x / 2) {}
+  __device__ __forceinline__ bool at(const TcGroup& G, TileCoord* tcd) const { return pair_tile_at(G, w, tcd); }
+  __device__ __forceinline__ void step() { w += gridDim.x / 2; }
+};
+template <>
+struct PairWalk<true> {
+  Deal<BlockPair> deal;
+  int k;
+  __device__ __forceinline__ explicit PairWalk(const TcHeadGroup& G) : deal(G, blockIdx.x / 2, gridDim.x / 2, dynamic_rows(G)), k(0) {}
+  __device__ __forceinline__ bool at(const TcHeadGroup& G, TileCoord* tcd) const { return deal.at(G, k, tcd); }
+  __device__ __forceinline__ void step() { ++k; }
 };
 
 __device__ __forceinline__ float tanh_fast(float x) {
@@ -225,9 +312,8 @@ struct TmemAcc {
 // warps share the tile's 64-column panels, first and second half, and the epilogue takes half as long.  Each warp then
 // has one staging tile instead of two (the staging area is the same size).
 // EPI: what the instantiation can fuse besides bias, residual and the row reduction.
-enum { EPI_NONE = 0, EPI_ACT, EPI_ROPE, EPI_HEAD_STATS, EPI_HEAD_GRAD };
 template <int BN, int ESETS, int EPI, typename Acc, typename Wait>
-__device__ __forceinline__ bool epilogue_tile(const TcProblem& P, int m0, int n0, int slice, int q, Acc acc, uint32_t stg0, int& pc, Wait wait) {
+__device__ __forceinline__ bool epilogue_tile(const TcProblem& P, const HeadProblem* H, int m0, int n0, int slice, int q, Acc acc, uint32_t stg0, int& pc, Wait wait) {
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, set = (warp - 2) / 4;
   constexpr int PPS = BN / 64 / ESETS;              // panels per set
   const int row = m0 + q * 32 + lane;               // row of the problem owned by this thread
@@ -262,8 +348,8 @@ __device__ __forceinline__ bool epilogue_tile(const TcProblem& P, int m0, int n0
     }
   }
   float alpha = 1.f;
-  if constexpr (EPI == EPI_NONE) {
-    if (P.over) alpha = P.alpha / fmaxf(*P.over, 1.f);
+  if constexpr (EPI == EPI_HEAD_OUT) {
+    if (H->over) alpha = H->alpha / fmaxf(*H->over, 1.f);
   }
   if (!wait()) return false;
   tc::tc_fence_after();
@@ -276,7 +362,7 @@ __device__ __forceinline__ bool epilogue_tile(const TcProblem& P, int m0, int n0
     acc.load(pn * 64, *reinterpret_cast<uint32_t(*)[32]>(&v[0]));
     acc.load(pn * 64 + 32, *reinterpret_cast<uint32_t(*)[32]>(&v[32]));
     acc.wait();
-    if (P.sums) {
+    if (EPI == EPI_HEAD_OUT ? H->sums != 0 : P.ksplit > 1) {
       // partial sums of a reduction slice: two 32-column halves of the panel, fp32, added to the accumulation
       // buffer by bulk tensor reductions, or stored there (same staging tiles and swizzle as the bf16 rows below)
 #pragma unroll 1
@@ -292,9 +378,13 @@ __device__ __forceinline__ bool epilogue_tile(const TcProblem& P, int m0, int n0
         tc::fence_proxy_async();
         __syncwarp();
         if (lane == 0) {
-          const int panel = n / 64 + slice * P.slice_panels;
-          if (P.sums == 1) tc::tma_store_4d(&P.tacc, stg, 0, hf, m0 + q * 32, panel);
-          else tc::tma_reduce_add_4d(&P.tacc, stg, 0, hf, m0 + q * 32, panel);
+          if constexpr (EPI == EPI_HEAD_OUT) {
+            const int panel = n / 64 + slice * H->slice_panels;
+            if (H->sums == 1) tc::tma_store_4d(&P.tacc, stg, 0, hf, m0 + q * 32, panel);
+            else tc::tma_reduce_add_4d(&P.tacc, stg, 0, hf, m0 + q * 32, panel);
+          } else {
+            tc::tma_reduce_add_4d(&P.tacc, stg, 0, hf, m0 + q * 32, n / 64);
+          }
           tc::bulk_commit_group();
           if (ESETS == 1) tc::bulk_wait_group_read1();
         }
@@ -388,11 +478,9 @@ __device__ __forceinline__ bool epilogue_tile(const TcProblem& P, int m0, int n0
         continue;
       }
     }
-    if constexpr (EPI == EPI_NONE) {
-      if (P.over) {
+    if constexpr (EPI == EPI_HEAD_OUT) {
 #pragma unroll
-        for (int j = 0; j < 64; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * alpha);
-      }
+      for (int j = 0; j < 64; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * alpha);
     }
     bool bias_left = bias != nullptr;
     if constexpr (EPI == EPI_ROPE) {
@@ -487,10 +575,12 @@ __device__ __forceinline__ bool epilogue_tile(const TcProblem& P, int m0, int n0
 
 // The epilogue that an instantiation has.
 template <int BN, int ESETS, int EPI, typename Acc, typename Wait>
-__device__ __forceinline__ bool fused_epilogue_tile(const TcProblem& P, int m0, int n0, int slice, int q, Acc acc, uint32_t stg0, int& pc, Wait wait) {
-  if constexpr (EPI == EPI_HEAD_STATS) return head_stats_tile<BN>(P, m0, n0, q, acc, wait);
-  else if constexpr (EPI == EPI_HEAD_GRAD) return head_grad_tile<BN>(P, m0, n0, q, acc, stg0, pc, wait);
-  else return epilogue_tile<BN, ESETS, EPI>(P, m0, n0, slice, q, acc, stg0, pc, wait);
+__device__ __forceinline__ bool any_epilogue_tile(const GroupOf<EPI>& G, const TileCoord& t, int m0, int q, Acc acc, uint32_t stg0, int& pc, Wait wait) {
+  const TcProblem& P = G.p[t.prob];
+  if constexpr (EPI == EPI_HEAD_STATS) return head_stats_tile<BN>(G.epi, P.seq, P.t_pad, m0, t.n0, q, acc, wait);
+  else if constexpr (EPI == EPI_HEAD_GRAD) return head_grad_tile<BN>(G.epi, P, m0, t.n0, q, acc, stg0, pc, wait);
+  else if constexpr (EPI == EPI_HEAD_OUT) return epilogue_tile<BN, ESETS, EPI>(P, &G.h[t.prob], m0, t.n0, t.slice, q, acc, stg0, pc, wait);
+  else return epilogue_tile<BN, ESETS, EPI>(P, nullptr, m0, t.n0, 0, q, acc, stg0, pc, wait);
 }
 
 // Persistent kernel: one block per SM walks the work list with stride gridDim.x.  Warp 0 feeds the
@@ -498,7 +588,7 @@ __device__ __forceinline__ bool fused_epilogue_tile(const TcProblem& P, int m0, 
 // other accumulator (bias, residual, padding-row mask, bf16 rows in R-Tile order), so the epilogue of
 // one tile overlaps the main loop of the next.
 template <int BN, int STAGES, int ESETS, int EPI>
-__global__ void __maxnreg__(ESETS == 2 ? 168 : EPI == EPI_ACT ? 255 : 224) gemm_tc_kernel(const __grid_constant__ TcGroup G) {
+__global__ void __maxnreg__(ESETS == 2 ? 168 : EPI == EPI_ACT ? 255 : 224) gemm_tc_kernel(const __grid_constant__ GroupOf<EPI> G) {
   using SP = SmemPlan<BN, STAGES>;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (tc::smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -549,8 +639,8 @@ __global__ void __maxnreg__(ESETS == 2 ? 168 : EPI == EPI_ACT ? 255 : 224) gemm_
     // Weights do not depend on the kernel before this one: their tiles for the first stages of the first
     // output tile are requested before waiting for that kernel, hiding their (cold) latency.
     int prefilled = 0;
-    const Deal<OneBlock<BN>> deal(G, blockIdx.x, gridDim.x, dynamic_rows(G));
-    if (deal.at(G, 0, &tcd) && G.p[tcd.prob].b_static && G.p[tcd.prob].ksplit == 1) {
+    Walk<BN, IS_HEAD<EPI>> walk(G);
+    if (walk.at(G, &tcd) && G.p[tcd.prob].b_static && G.p[tcd.prob].ksplit == 1) {
       const TcProblem& P = G.p[tcd.prob];
       if (leader) { tc::tma_prefetch_desc(&P.ta[0]); tc::tma_prefetch_desc(&P.tb[0]); }
       const int n = P.kblocks[0] < STAGES ? P.kblocks[0] : STAGES;
@@ -565,7 +655,7 @@ __global__ void __maxnreg__(ESETS == 2 ? 168 : EPI == EPI_ACT ? 255 : 224) gemm_
     }
     pdl_wait();
     if (G.late_trigger && leader) late_trigger(G);
-    for (int k = 0; ok && deal.at(G, k, &tcd); ++k) {
+    for (; ok && walk.at(G, &tcd); walk.step()) {
       const TcProblem& P = G.p[tcd.prob];
       for (int t = 0; t < P.n_terms && ok; ++t) {
         int kb = t == 0 ? tcd.kb0 : 0;
@@ -604,8 +694,7 @@ __global__ void __maxnreg__(ESETS == 2 ? 168 : EPI == EPI_ACT ? 255 : 224) gemm_
     bool ok = true;
     TileCoord tcd;
     const uint32_t hi = tc::smem_desc_hi(1024);
-    const Deal<OneBlock<BN>> deal(G, blockIdx.x, gridDim.x, dynamic_rows(G));
-    for (; ok && deal.at(G, ti, &tcd); ++ti) {
+    for (Walk<BN, IS_HEAD<EPI>> walk(G); ok && walk.at(G, &tcd); walk.step(), ++ti) {
       const TcProblem& P = G.p[tcd.prob];
       const int ab = ti & 1;
       if (!tc::mbar_wait_warp(acc_empty(ab), ((ti >> 1) & 1) ^ 1, status, 104)) { ok = false; break; }
@@ -640,14 +729,12 @@ __global__ void __maxnreg__(ESETS == 2 ? 168 : EPI == EPI_ACT ? 255 : 224) gemm_
     pdl_wait();                                       // the previous kernel may still be reading what we overwrite
     group_chores(G, threadIdx.x - 64, 128 * ESETS);
     const int q = warp % 4;                           // the TMEM lane quarter this warp may access
-    const Deal<OneBlock<BN>> deal(G, blockIdx.x, gridDim.x, dynamic_rows(G));
     int ti = 0, pc = 0;                               // tiles and panels done by this warp
     bool ok = true;
     TileCoord tcd;
-    for (; ok && deal.at(G, ti, &tcd); ++ti) {
-      const TcProblem& P = G.p[tcd.prob];
+    for (Walk<BN, IS_HEAD<EPI>> walk(G); ok && walk.at(G, &tcd); walk.step(), ++ti) {
       const int ab = ti & 1;
-      const bool ready = fused_epilogue_tile<BN, ESETS, EPI>(P, tcd.m0, tcd.n0, tcd.slice, q, TmemAcc{tmem_base + ((uint32_t)(q * 32) << 16) + ab * BN}, base + SP::STG_OFF, pc, [&] {
+      const bool ready = any_epilogue_tile<BN, ESETS, EPI>(G, tcd, tcd.m0, q, TmemAcc{tmem_base + ((uint32_t)(q * 32) << 16) + ab * BN}, base + SP::STG_OFF, pc, [&] {
         return tc::mbar_wait(acc_full(ab), (ti >> 1) & 1, status, 103);
       });
       if (!ready) { ok = false; break; }
@@ -680,7 +767,7 @@ struct PairSmem {
 };
 
 template <int EPI>
-__global__ void __cluster_dims__(2, 1, 1) __maxnreg__(EPI == EPI_ACT ? 255 : 224) gemm_tc_pair_kernel(const __grid_constant__ TcGroup G) {
+__global__ void __cluster_dims__(2, 1, 1) __maxnreg__(EPI == EPI_ACT ? 255 : 224) gemm_tc_pair_kernel(const __grid_constant__ GroupOf<EPI> G) {
   using SP = PairSmem;
   constexpr int STAGES = PAIR_STAGES, BN = PAIR_BN;
   extern __shared__ uint8_t smem_raw[];
@@ -693,7 +780,6 @@ __global__ void __cluster_dims__(2, 1, 1) __maxnreg__(EPI == EPI_ACT ? 255 : 224
   const uint32_t slot = bars + 8 * SP::N_BARS;
   const int warp = (int)tc::uniform(threadIdx.x / 32), lane = threadIdx.x % 32;
   const uint32_t rank = tc::cluster_ctarank();
-  const int pair_id = blockIdx.x / 2, n_pairs = gridDim.x / 2;
   const tc::Status status(G.status, G.reset_status);
   constexpr uint32_t TMEM_COLS = 2 * BN;
 
@@ -731,8 +817,7 @@ __global__ void __cluster_dims__(2, 1, 1) __maxnreg__(EPI == EPI_ACT ? 255 : 224
     const uint32_t full0 = tc::map_to_cta(full(0), 0);
     pdl_wait();
     if (G.late_trigger && leader) late_trigger(G);
-    const Deal<BlockPair> deal(G, pair_id, n_pairs, dynamic_rows(G));
-    for (int k = 0; ok && deal.at(G, k, &tcd); ++k) {
+    for (PairWalk<IS_HEAD<EPI>> walk(G); ok && walk.at(G, &tcd); walk.step()) {
       const TcProblem& P = G.p[tcd.prob];
       const int m0 = tcd.m0 + (int)rank * 128, n0 = tcd.n0 + (int)rank * 128;
       for (int t = 0; t < P.n_terms && ok; ++t) {
@@ -763,8 +848,7 @@ __global__ void __cluster_dims__(2, 1, 1) __maxnreg__(EPI == EPI_ACT ? 255 : 224
     bool ok = true;
     TileCoord tcd;
     const uint32_t hi = tc::smem_desc_hi(1024);
-    const Deal<BlockPair> deal(G, pair_id, n_pairs, dynamic_rows(G));
-    for (; ok && deal.at(G, ti, &tcd); ++ti) {
+    for (PairWalk<IS_HEAD<EPI>> walk(G); ok && walk.at(G, &tcd); walk.step(), ++ti) {
       const TcProblem& P = G.p[tcd.prob];
       const int ab = ti & 1;
       if (!tc::mbar_wait_warp(acc_empty(ab), ((ti >> 1) & 1) ^ 1, status, 114)) { ok = false; break; }
@@ -797,15 +881,13 @@ __global__ void __cluster_dims__(2, 1, 1) __maxnreg__(EPI == EPI_ACT ? 255 : 224
     pdl_wait();
     group_chores(G, threadIdx.x - 64, 128);
     const int q = warp % 4;
-    const Deal<BlockPair> deal(G, pair_id, n_pairs, dynamic_rows(G));
     int ti = 0, pc = 0;
     bool ok = true;
     TileCoord tcd;
-    for (; ok && deal.at(G, ti, &tcd); ++ti) {
-      const TcProblem& P = G.p[tcd.prob];
+    for (PairWalk<IS_HEAD<EPI>> walk(G); ok && walk.at(G, &tcd); walk.step(), ++ti) {
       const int ab = ti & 1;
       const int m0 = tcd.m0 + (int)rank * 128;
-      const bool ready = fused_epilogue_tile<BN, 1, EPI>(P, m0, tcd.n0, tcd.slice, q, TmemAcc{tmem_base + ((uint32_t)(q * 32) << 16) + ab * BN}, base + SP::STG_OFF, pc, [&] {
+      const bool ready = any_epilogue_tile<BN, 1, EPI>(G, tcd, m0, q, TmemAcc{tmem_base + ((uint32_t)(q * 32) << 16) + ab * BN}, base + SP::STG_OFF, pc, [&] {
         return tc::mbar_wait(acc_full(ab), (ti >> 1) & 1, status, 113);
       });
       if (!ready) { ok = false; break; }
@@ -881,7 +963,7 @@ __global__ void __launch_bounds__(320, 1) gemm_tc_split_kernel(const __grid_cons
 
   const int slice = blockIdx.x % G.slices;
   TileCoord tcd;
-  Deal<OneBlock<BN>>(G, blockIdx.x / G.slices, 1 << 20, 0).at(G, 0, &tcd);
+  tile_at<BN>(G, blockIdx.x / G.slices, &tcd);
   const TcProblem& P = G.p[tcd.prob];
   int total = 0;
   for (int t = 0; t < P.n_terms; ++t) total += P.kblocks[t];
@@ -1000,7 +1082,7 @@ __global__ void __launch_bounds__(320, 1) gemm_tc_split_kernel(const __grid_cons
     const int rg = slice * groups + q;                   // the row group this warp finishes (the first `groups` warps of a set)
     int pc = 0;
     if (q < groups && tcd.m0 + rg * 32 < P.m)
-      epilogue_tile<BN, 2, EPI>(P, tcd.m0, tcd.n0, 0, rg, PartialAcc{base + (rg * 32 + lane) * SPLIT_LD * 4}, base + SP::STG_OFF, pc, exchange);
+      epilogue_tile<BN, 2, EPI>(P, nullptr, tcd.m0, tcd.n0, 0, rg, PartialAcc{base + (rg * 32 + lane) * SPLIT_LD * 4}, base + SP::STG_OFF, pc, exchange);
     else
       exchange();
     if (lane == 0) tc::bulk_wait_group0();
@@ -1162,17 +1244,10 @@ cudaError_t fill_group(TcGroup& G, const GemmArgs* gs, int count, int bn_box, in
     }
     P.m = g.m; P.n = g.n;
     if (g.epi != 6 && !fbl_encode_rtile_map(&P.tc, g.c, g.c_rpad, g.n / 64, 32, 1, g.c_rows)) return cudaErrorInvalidValue;   // one warp's rows
-    // with rows enough for one tile at most, the work list is known without the device's number
-    P.dyn = g.dyn == 1 && g.m <= tile_m ? 0 : g.dyn;
-    G.dynamic |= P.dyn;
-    if (g.dyn && (!g.rows || g.n_terms != 1 || g.rows != gs[0].rows || (g.dyn == 2 && g.ksplit > 1))) return cudaErrorInvalidValue;
     P.b_static = g.b_static;
     P.c_rpad = g.c_rpad; P.seq = g.seq; P.t_pad = g.t_pad;
     P.dot_hd = g.dot_hd; P.dot_hq = g.dot_hq; P.epi = g.epi;
-    if (g.epi >= 6) {
-      if (g.epi > 7 || g.ksplit > 1 || g.acc_mode || g.n_terms != 1 || g.bias || g.residual || g.dot_with || !g.head.ids || !g.head.count || !g.head.row_of || !g.head.n || !g.rows)
-        return cudaErrorInvalidValue;
-    } else if (g.epi != 0) {
+    if (g.epi != 0 && g.epi < 6) {
       const bool rope = g.epi == 5, two_out = g.epi != 2 && !rope;
       if (g.epi < 1 || g.epi > 5 || g.ksplit > 1 || g.dot_with || (g.epi >= 2 && !rope && !g.residual) || (g.epi == 4 && !g.aux1) ||
           (two_out && !g.c2) || (rope && (!g.rope || g.residual || g.t_pad <= 0)))
@@ -1184,8 +1259,6 @@ cudaError_t fill_group(TcGroup& G, const GemmArgs* gs, int count, int bn_box, in
       if (g.n_terms != 1 || g.bias || g.residual || g.dot_with || g.t_pad > 0 || !g.acc) return cudaErrorInvalidValue;
       const int slices = g.ksplit > 1 ? g.ksplit : 1, per = (P.kblocks[0] + slices - 1) / slices;        // no empty slice
       P.ksplit = (P.kblocks[0] + per - 1) / per;
-      P.sums = g.acc_mode == 1 ? 1 : 2;
-      P.slice_panels = g.acc_mode ? g.n / 64 : 0;
       if (!fbl_encode_f32_panel_map(&P.tacc, g.acc, g.c_rpad, g.acc_mode ? g.n / 64 * P.ksplit : g.n / 64, 32, 1)) return cudaErrorInvalidValue;
     }
     tiles += ((g.m + tile_m - 1) / tile_m) * ((g.n + tile_n - 1) / tile_n) * P.ksplit;
@@ -1200,7 +1273,7 @@ namespace {
 int group_epi(const GemmArgs* gs, int count) {
   int epi = EPI_NONE;
   for (int i = 0; i < count; ++i)
-    if (gs[i].epi != 0) epi = gs[i].epi == 5 ? EPI_ROPE : gs[i].epi == 6 ? EPI_HEAD_STATS : gs[i].epi == 7 ? EPI_HEAD_GRAD : EPI_ACT;
+    if (gs[i].epi != 0) epi = gs[i].epi == 5 ? EPI_ROPE : EPI_ACT;
   return epi;
 }
 
@@ -1220,21 +1293,17 @@ cudaError_t group_launch(GroupLaunch& L, void (*k)(const TcGroup), int grid, int
   return cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
 }
 
-bool point_group(GroupLaunch& L, const GemmArgs* gs, int32_t* status) {
-  TcGroup& G = L.G;
+bool point_group(TcGroup& G, const int* order, const GemmArgs* gs, int32_t* status) {
   G.status = status;
-  G.rows = gs[0].rows;
   G.zero_ptr = (uint4*)gs[0].zero_ptr; G.zero_vec = (long long)(gs[0].zero_bytes / 16); G.reset_status = gs[0].reset_status;
   bool ok = true;
   for (int i = 0; i < G.count; ++i) {
-    const GemmArgs& g = gs[L.order[i]];
+    const GemmArgs& g = gs[order[i]];
     TcProblem& P = G.p[i];
     for (int t = 0; t < P.n_terms; ++t) ok = ok && fbl_map_set_base(&P.ta[t], g.t[t].a) && fbl_map_set_base(&P.tb[t], g.t[t].b);
     if (P.epi != 6) ok = ok && fbl_map_set_base(&P.tc, g.c);
     if (P.epi != 0 && P.epi != 2 && P.epi < 5) ok = ok && fbl_map_set_base(&P.tc2, g.c2);
-    if (P.sums) ok = ok && fbl_map_set_base(&P.tacc, g.acc);
-    P.head = g.head;
-    P.over = g.over; P.alpha = g.alpha;
+    if (P.ksplit > 1 || g.ksplit > 1 || g.acc_mode) ok = ok && fbl_map_set_base(&P.tacc, g.acc);
     P.c = (__nv_bfloat16*)g.c; P.bias = g.bias; P.residual = (const __nv_bfloat16*)g.residual;
     P.dot_with = (const __nv_bfloat16*)g.dot_with; P.dot_out = g.dot_out;
     P.aux1 = (const __nv_bfloat16*)g.aux1; P.rope = g.rope;
@@ -1260,21 +1329,6 @@ cudaError_t make_group_bn(GroupLaunch& L, const fbl_plan* p, const GemmArgs* gs,
     default: k = two_sets ? gemm_tc_kernel<BN, STAGES, SETS, EPI_NONE> : gemm_tc_kernel<BN, STAGES, 1, EPI_NONE>;
   }
   return group_launch(L, k, grid, two_sets ? 320 : 192, SmemPlan<BN, STAGES>::TOTAL, gs[0].serial);
-}
-
-// The head's products: 256 columns to a tile (a partial of the softmax statistics is a tile's), on one CTA or a pair.
-cudaError_t make_group_head(GroupLaunch& L, const fbl_plan* p, const GemmArgs* gs, int count, bool pair) {
-  int tiles = 0;
-  if (count != 1) return cudaErrorInvalidValue;
-  const bool stats = gs[0].epi == 6;
-  cudaError_t e = fill_group(L.G, gs, count, pair ? 128 : 256, pair ? 256 : BM, 256, &tiles);
-  if (e != cudaSuccess) return e;
-  if (pair) {
-    const int pairs = tiles < p->sm_count / 2 ? tiles : p->sm_count / 2;
-    return group_launch(L, stats ? gemm_tc_pair_kernel<EPI_HEAD_STATS> : gemm_tc_pair_kernel<EPI_HEAD_GRAD>, 2 * pairs, 192, PairSmem::TOTAL, gs[0].serial);
-  }
-  return group_launch(L, stats ? gemm_tc_kernel<256, 4, 1, EPI_HEAD_STATS> : gemm_tc_kernel<256, 4, 1, EPI_HEAD_GRAD>,
-                      tiles < p->sm_count ? tiles : p->sm_count, 192, SmemPlan<256, 4>::TOTAL, gs[0].serial);
 }
 
 cudaError_t make_group_split(GroupLaunch& L, const GemmArgs* gs, int count, int slices) {
@@ -1420,28 +1474,6 @@ static cudaError_t make_group(GroupLaunch& L, const fbl_plan* p, const GemmArgs*
     w[i] = {gs[i].m, gs[i].n, 0, gs[i].ksplit > 1 ? gs[i].ksplit : 1};
     for (int t = 0; t < gs[i].n_terms; ++t) w[i].kb += (gs[i].t[t].k + BK - 1) / BK;
   }
-  if (gs[0].epi >= 6) {
-    const double one = tile_makespan(TILE_COST[TILE_WIDE], w, count, p->sm_count), two = tile_makespan(TILE_COST[TILE_PAIR], w, count, p->sm_count / 2);
-    return make_group_head(L, p, gs, count, pair_mode >= 0 ? pair_mode == 1 : two < one);
-  }
-  if (gs[0].rows && count == 2) {
-    // dX's slices and dW's tiles, or the other way round: the longer ones first
-    const int first = w[1].kb / w[1].split > w[0].kb / w[0].split ? 1 : 0;
-    const TileWork a = w[first], b = w[1 - first];
-    double clocks;
-    kind = best_deal(a, b, p->sm_count, pair_mode != 0, &clocks);
-    if (two_sets_pay(TILE_COST[TILE_WIDE], b)) kind = TILE_WIDE;
-    if (pair_mode == 1) kind = TILE_PAIR;
-    for (int i = 0; i < 2; ++i) { L.order[i] = i ? 1 - first : first; by_length[i] = gs[L.order[i]]; }
-    by_length[0].serial = gs[0].serial; by_length[0].late_trigger = gs[0].late_trigger;
-    const TileCost& c = TILE_COST[kind];
-    const bool two = two_sets_pay(c, b);
-    cudaError_t e = kind == TILE_PAIR ? make_group_pair(L, p, by_length, 2)
-                    : kind == TILE_WIDE ? make_group_bn<256, 4>(L, p, by_length, 2, two ? 2 : 0) : make_group_bn<128, 6>(L, p, by_length, 2, two ? 2 : 0);
-    L.idle = 0;
-    L.G.kb_clocks = (float)c.kb; L.G.unit_clocks = (float)c.unit; L.G.floor_clocks = (float)(two ? 0.5 * c.epilogue : c.epilogue);
-    return e;
-  }
   if (pair_mode == 1) {
     kind = TILE_PAIR;
   } else if (ch.bn) {
@@ -1453,7 +1485,7 @@ static cudaError_t make_group(GroupLaunch& L, const fbl_plan* p, const GemmArgs*
       const double t = tile_makespan(TILE_COST[TILE_SLIM], w, count, p->sm_count);
       if (t < clocks) { clocks = t; kind = TILE_SLIM; }
     }
-    const int slices = gs[0].rows ? 0 : best_slices(w, count, p->sm_count, clocks);       // (a slice needs a k-block)
+    const int slices = best_slices(w, count, p->sm_count, clocks);
     if (slices) {
       L.idle = 1 << 20;                              // fewer blocks than SMs, as a rule
       return make_group_split(L, gs, count, slices);
@@ -1494,7 +1526,7 @@ cudaError_t launch_gemm_tc_group(const fbl_plan* p, const GemmArgs* gs, int coun
   key.add(ch.esets, 0);
   return LaunchMemo<GroupLaunch, 12>::run(p, FBL_MEMO_TC_GEMM, key,
       [&](GroupLaunch& L) { return make_group(L, p, gs, count, ch); },
-      [&](GroupLaunch& L) { return point_group(L, gs, status); },
+      [&](GroupLaunch& L) { return point_group(L.G, L.order, gs, status); },
       [&](const GroupLaunch& L) {
         if (gs[0].late_trigger) *gs[0].late_trigger = L.idle;
         if (L.cluster) return launch_cluster(L.kernel, dim3(L.grid), dim3(L.threads), L.smem, st, L.cluster, !L.serial, L.G);
@@ -1531,6 +1563,91 @@ int gemm_tc_choose_split(int sm_count, const GemmShape* sh, int count, bool zero
     else if (cost < (zero_rides ? 0.9 : 0.85) * base_cost && cost < best_cost) { best = S; best_cost = cost; }   // worth it only with a clear gain
   }
   return best;
+}
+
+namespace {
+
+struct HeadLaunch {
+  TcHeadGroup G;
+  int order[2], grid, threads;
+  size_t smem;
+  void (*kernel)(const TcHeadGroup);
+};
+
+// The head's products: 256 columns to a tile where a partial of the softmax statistics is a tile's, on one CTA or a pair; dX beside dW.
+cudaError_t make_head(HeadLaunch& L, const fbl_plan* p, const GemmArgs* gs, int count) {
+  TileWork w[2];
+  for (int i = 0; i < count; ++i) w[i] = {gs[i].m, gs[i].n, (gs[i].t[0].k + BK - 1) / BK, gs[i].ksplit > 1 ? gs[i].ksplit : 1};
+  int kind = TILE_WIDE, sets = 1;
+  bool balanced = false;
+  L.order[0] = 0; L.order[1] = 1;
+  const int pair_mode = p->knob_gemm_pair;
+  if (gs[0].epi) {
+    const double one = tile_makespan(TILE_COST[TILE_WIDE], w, 1, p->sm_count), two = tile_makespan(TILE_COST[TILE_PAIR], w, 1, p->sm_count / 2);
+    // (a tie goes to pairs, which read W once for 256 rows: 256 tokens of 1024 over 50257 columns 35 -> 30 us a product)
+    if (pair_mode >= 0 ? pair_mode == 1 : two < 1.02 * one) kind = TILE_PAIR;
+  } else if (count == 2) {
+    // dX's slices and dW's tiles, or the other way round: the longer ones first
+    if (w[1].kb / w[1].split > w[0].kb / w[0].split) { std::swap(w[0], w[1]); L.order[0] = 1; L.order[1] = 0; }
+    double clocks;
+    kind = best_deal(w[0], w[1], p->sm_count, pair_mode != 0, &clocks);
+    if (two_sets_pay(TILE_COST[TILE_WIDE], w[1])) kind = TILE_WIDE;
+    balanced = true;
+  } else {
+    double clocks;
+    kind = best_tile(w, 1, p->sm_count, pair_mode != 0, &clocks);
+  }
+  if (!gs[0].epi && pair_mode == 1) kind = TILE_PAIR;
+  const TileCost& c = TILE_COST[kind];
+  GemmArgs sorted[2];
+  for (int i = 0; i < count; ++i) sorted[i] = gs[L.order[i]];
+  int units = 0;
+  memset(static_cast<void*>(&L.G), 0, sizeof(L.G));
+  cudaError_t e = fill_group(L.G, sorted, count, kind == TILE_PAIR ? 128 : c.n, c.m, c.n, &units);
+  if (e != cudaSuccess) return e;
+  const bool two = !gs[0].epi && kind != TILE_PAIR && (balanced ? two_sets_pay(c, w[1]) : units <= p->sm_count);
+  if (two || (!gs[0].epi && kind != TILE_PAIR && units <= p->sm_count)) sets = 2;
+  for (int i = 0; i < count; ++i) {
+    const GemmArgs& g = sorted[i];
+    HeadProblem& H = L.G.h[i];
+    if (!g.rows || g.rows != gs[0].rows || g.n_terms != 1 || g.bias || g.residual || g.dot_with || (g.dyn == 2 && g.ksplit > 1)) return cudaErrorInvalidValue;
+    // with rows enough for one tile at most, the work list is known without the device's number
+    H.dyn = g.dyn == 1 && g.m <= c.m ? 0 : g.dyn;
+    L.G.dynamic |= H.dyn;
+    H.sums = g.acc_mode;
+    H.slice_panels = g.n / 64;
+  }
+  if (balanced) { L.G.kb_clocks = (float)c.kb; L.G.unit_clocks = (float)c.unit; L.G.floor_clocks = (float)(two ? 0.5 * c.epilogue : c.epilogue); }
+  const int slots = kind == TILE_PAIR ? p->sm_count / 2 : p->sm_count;
+  L.grid = (units < slots ? units : slots) * (kind == TILE_PAIR ? 2 : 1);
+  L.threads = sets == 2 ? 320 : 192;
+  L.smem = kind == TILE_PAIR ? (size_t)PairSmem::TOTAL : kind == TILE_WIDE ? (size_t)SmemPlan<256, 4>::TOTAL : (size_t)SmemPlan<128, 6>::TOTAL;
+  if (kind == TILE_PAIR)
+    L.kernel = gs[0].epi == 6 ? gemm_tc_pair_kernel<EPI_HEAD_STATS> : gs[0].epi == 7 ? gemm_tc_pair_kernel<EPI_HEAD_GRAD> : gemm_tc_pair_kernel<EPI_HEAD_OUT>;
+  else if (gs[0].epi)
+    L.kernel = gs[0].epi == 6 ? gemm_tc_kernel<256, 4, 1, EPI_HEAD_STATS> : gemm_tc_kernel<256, 4, 1, EPI_HEAD_GRAD>;
+  else if (kind == TILE_WIDE)
+    L.kernel = sets == 2 ? gemm_tc_kernel<256, 4, 2, EPI_HEAD_OUT> : gemm_tc_kernel<256, 4, 1, EPI_HEAD_OUT>;
+  else
+    L.kernel = sets == 2 ? gemm_tc_kernel<128, 6, 2, EPI_HEAD_OUT> : gemm_tc_kernel<128, 6, 1, EPI_HEAD_OUT>;
+  return cudaFuncSetAttribute(L.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)L.smem);
+}
+
+}  // namespace
+
+cudaError_t launch_gemm_tc_head(const fbl_plan* p, const GemmArgs* gs, int count, int32_t* status, cudaStream_t st) {
+  if (count < 1 || count > 2 || (gs[0].epi && (count != 1 || gs[0].epi < 6 || gs[0].epi > 7))) return cudaErrorInvalidValue;
+  LaunchKey key;
+  gemm_group_key(key, gs, count);
+  return LaunchMemo<HeadLaunch, 12>::run(p, FBL_MEMO_TC_GEMM, key,
+      [&](HeadLaunch& L) { return make_head(L, p, gs, count); },
+      [&](HeadLaunch& L) {
+        for (int i = 0; i < count; ++i) { L.G.h[i].over = gs[L.order[i]].over; L.G.h[i].alpha = gs[L.order[i]].alpha; }
+        L.G.rows = gs[0].rows;
+        L.G.epi = gs[0].head;
+        return point_group(L.G, L.order, gs, status);
+      },
+      [&](const HeadLaunch& L) { return launch_pdl(L.kernel, dim3(L.grid), dim3(L.threads), L.smem, st, L.G); });
 }
 
 int gemm_tc_choose_own_slices(int sm_count, const GemmShape* dw, const GemmShape& dx) {

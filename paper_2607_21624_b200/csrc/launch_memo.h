@@ -15,7 +15,7 @@
 #include "fbl_internal.h"
 
 struct LaunchKey {
-  static constexpr int MAX = 144;          // five products of four terms are 129 words
+  static constexpr int MAX = 128;          // five products of four terms are 99 words
   uint64_t v[MAX];
   int n = 0;
   LaunchKey() {                            // function attributes are a device's
@@ -76,12 +76,11 @@ inline void gemm_group_key(LaunchKey& k, const GemmArgs* gs, int count) {
       const GemmTerm& m = g.t[t];
       k.add((uint64_t)m.a_rpad); k.add((uint64_t)m.b_rpad);
       k.add(m.k, m.a_trans * 2 + m.b_trans);
-      k.add((uint64_t)m.b_rows);
     }
-    k.add((uint64_t)g.c_rows); k.add(g.acc_mode, g.dyn);
     k.add((uint64_t)g.c_rpad); k.add(g.seq, g.t_pad); k.add(g.dot_hd, g.dot_hq); k.add(g.ksplit, g.epi);
     // which operands there are: fill_group's checks look at them
     k.add((g.bias != nullptr) | (g.residual != nullptr) << 1 | (g.dot_with != nullptr) << 2 | (g.aux1 != nullptr) << 3 |
           (g.c2 != nullptr) << 4 | (g.rope != nullptr) << 5 | (g.acc != nullptr) << 6, 0);
+    if (g.rows) { k.add((uint64_t)g.t[0].b_rows); k.add((uint64_t)g.c_rows); k.add(g.acc_mode, g.dyn); }       // the head's
   }
 }

@@ -119,7 +119,7 @@ def refused(code, make):
 @pytest.mark.parametrize("kw,code", [
     (dict(batch=0), -1), (dict(seq=0), -1), (dict(seq=-3), -1), (dict(d_model=0), -1), (dict(vocab=0), -1), (dict(vocab=-5), -1),
     (dict(top_k=-1), -1), (dict(temperature=0.0), -1), (dict(temperature=-1.0), -1), (dict(temperature=float("nan")), -1),
-    (dict(temperature=float("inf"), top_k=4), -1), (dict(temperature=2.0), -1),
+    (dict(temperature=float("inf"), top_k=4), -1), (dict(temperature=1e-39, top_k=4), -1), (dict(temperature=2.0), -1),
     (dict(d_model=96), -2), (dict(d_model=16448), -2), (dict(vocab=(1 << 20) + 1), -2), (dict(top_k=129), -2), (dict(batch=1 << 20, seq=8), -2),
 ])
 def test_head_plan_refusals(kw, code):
