@@ -456,7 +456,8 @@ int64_t fbl_norm_launch_count(const fbl_norm_plan* plan);
  * dloss [batch * seq] fp32, the gradient of each token's loss, or NULL: 1 / total[1], the gradient of the mean.  dX or dW may be
  * NULL: then that gradient is not formed (a frozen head; a frozen model).  The backward takes the X and W that the forward
  * had, and from `saved` the targets' entries, the softmax statistics and the rows of X with a loss, which the forward has brought
- * together there; `saved` serves any number of backward calls.
+ * together there; `saved` serves any number of backward calls.  Outputs overlap no input and no workspace (dW is written while W
+ * is still read).
  * bf16 storage: products on bf16 operands with fp32 sums; statistics, losses and gradients in fp32, dz rounded to bf16 as an
  * operand of the last two products.  The sums of dX over pieces and slices of the vocabulary are fp32, in a fixed order.
  * FBL_HEAD_PIECE and FBL_HEAD_SLICES, read at plan creation, override the columns of a piece and the slices of dX's reduction

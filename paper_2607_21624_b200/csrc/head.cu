@@ -215,6 +215,7 @@ int fbl_head_plan_create(const fbl_head_desc* desc, fbl_head_plan** out) {
       want = gemm_tc_f32_choose_areas(base, gs, 2);
     }
     if (getenv("FBL_HEAD_SLICES") && atoi(getenv("FBL_HEAD_SLICES")) > 0) want = atoi(getenv("FBL_HEAD_SLICES"));               // likewise
+    if (want > kb) want = kb;
     const int per = (kb + want - 1) / want;                                                                                   // none empty
     p->slices = (kb + per - 1) / per;
   }
