@@ -109,8 +109,8 @@ struct HeadEpi {
   long long rows;               // pitch of every per-row array here
   int vocab, col0, top_k;       // columns of the vocabulary, the first one of this product's, entries a row has at most
   float scale;                  // from a product to a logit times log2 e
-  float2* part;                 // forward: [row][column tile, `tiles` of them] (k, sum of 2^((product - k) scale))
-  int tiles;
+  float2* part;                 // forward: [row][columns' part, `tiles` of them] (k, sum of 2^((product - k) scale))
+  int tiles, tile;              // tile: which a bf16 product is cut into (gemm_tc_logits_tile; backward -1: by its own size)
   float* z_at;                  // forward: [entry][row] the products at the targets
   const float *k, *sum;         // backward: the row's k and sum
   const float *dloss, *over;    // backward: the gradient of each token's loss [batch * seq], or else 1 / max(*over, 1), or else 1
@@ -192,12 +192,14 @@ struct GemmShape { int64_t m; int n; int kblocks; int splittable; };
 int gemm_tc_choose_split(int sm_count, const GemmShape* sh, int count, bool zero_rides);
 // The head's products: one with an epilogue of the vocabulary's softmax, or dX and dW, or one of them.
 cudaError_t launch_gemm_tc_head(const fbl_plan* p, const GemmArgs* gs, int count, int32_t* status, cudaStream_t st);
-// The same for slices with areas of their own, of dX beside dW (which may be null).
+// The tile of the forward's product (HeadEpi.tile; `knob` >= 0: that one), and how many columns a partial of the statistics then has.
+int gemm_tc_logits_tile(const fbl_plan* p, int64_t m, int n, int k, int knob, int* width);
+// gemm_tc_choose_split for slices with areas of their own, of dX beside dW (which may be null).
 int gemm_tc_choose_own_slices(int sm_count, const GemmShape* dw, const GemmShape& dx);
 cudaError_t launch_gemm_tc_f32_head(const fbl_plan* p, const GemmArgs* gs, int count, int32_t* status, cudaStream_t st);
 // Areas of an fp32 group's last problem, whose other fields but addresses are set.
 int gemm_tc_f32_choose_areas(const fbl_plan* p, GemmArgs* gs, int count);
-constexpr int HEAD_TILE = 256, HEAD_TILE_F32 = 64;      // columns of a partial of the softmax statistics
+constexpr int HEAD_TILE = 256, HEAD_TILE_F32 = 64;      // pieces of the vocabulary are whole tiles of 256 columns; an fp32 partial of the statistics
 cudaError_t launch_wait_timeout_selftest(int32_t* status, long long limit_cycles, cudaStream_t st);
 // With less than a tile of token rows on either side a bf16 layer keeps P and dS in fp32, or in two bf16 values: their rounding
 // is as large as that of the results there (dQ, dK, dV off by 2.3e-3 of their norm instead of 1.65e-3), and with the rotary

@@ -61,6 +61,7 @@ struct fbl_head_plan {
   int cols;                     // vocabulary in whole tiles: columns of the logits
   int64_t w_rows;               // stored rows of W
   int top_k, tiles;             // entries a row; partials of the softmax statistics
+  int logits_tile, grad_tile;   // HeadEpi.tile of the two passes
   int piece, pieces, slices;    // columns of a piece; pieces; areas that dX's reduction is cut into
   float scale;                  // from a product to a logit times log2 e
   size_t sv_ids, sv_y, sv_count, sv_constant, sv_row_of, sv_pos, sv_n, sv_k, sv_sum, sv_total, sv_x, saved_bytes;
@@ -159,6 +160,7 @@ int forward(const fbl_head_plan* p, const void* W, float* loss, float* total, co
   g.epi = 6;
   g.head = epilogue_of(p, R, 0);
   g.head.part = part; g.head.tiles = p->tiles; g.head.z_at = z_at;
+  g.head.tile = p->logits_tile;
   HEAD_RUN(run_products(p, &g, 1, status, st));
   HEAD_STEP(launch_head_combine(part, p->tiles, z_at, R, p->scale, loss, total, (float*)(sf + p->sf_blocks), p->d.seq, p->base->t_pad, status, st));
   return FBL_OK;
@@ -192,7 +194,11 @@ int fbl_head_plan_create(const fbl_head_desc* desc, fbl_head_plan** out) {
   p->cols = (int)up(d.vocab, base->tw);
   p->w_rows = d.vocab_rows ? up(d.vocab, 8) : d.d_model;
   p->top_k = d.top_k ? d.top_k : 1;
-  p->tiles = bf16 ? (p->cols + HEAD_TILE - 1) / HEAD_TILE : (p->cols + HEAD_TILE_F32 - 1) / HEAD_TILE_F32;
+  int width = HEAD_TILE_F32;
+  p->grad_tile = getenv("FBL_HEAD_TILE") ? atoi(getenv("FBL_HEAD_TILE")) : -1;                                               // tuning / test knob
+  p->logits_tile = bf16 ? gemm_tc_logits_tile(base, p->n_pad, p->cols, d.d_model, p->grad_tile, &width) : 0;
+  if (p->grad_tile >= 0) p->grad_tile = p->logits_tile;
+  p->tiles = (p->cols + width - 1) / width;
   p->scale = (float)(1.4426950408889634 / (double)d.temperature * (1.0 + (bf16 ? logit_lift(d.d_model) : 0.0)));
 
   // pieces of about one size, in whole tiles
@@ -355,6 +361,7 @@ int fbl_head_bwd(const fbl_head_plan* p, const void* X, const void* W, const flo
       g.epi = 7;
       g.head = epilogue_of(p, R, col0);
       g.head.dloss = dloss;
+      g.head.tile = p->grad_tile;
       if (!bf16) g.head.over = over;
       HEAD_RUN(run_products(p, &g, 1, status, st));
     }

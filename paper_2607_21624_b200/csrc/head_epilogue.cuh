@@ -26,13 +26,19 @@ namespace headepi {
 
 constexpr int NONE = 0x7fffffff;
 
-// The row's entries from column `col` on.
+// The row's entries from column `col` on.  What is read first goes out together: each step that waits for the one before costs a tile of
+// a short reduction some 700 clocks.
 struct Entries {
   const int32_t* ids;
   long long rows;
   int at, count, next;
   __device__ __forceinline__ Entries() : ids(nullptr), rows(0), at(0), count(0), next(NONE) {}
-  __device__ __forceinline__ Entries(const HeadEpi& H, int row, int count_, int col) : ids(H.ids + row), rows(H.rows), at(0), count(count_) {
+  __device__ __forceinline__ Entries(const HeadEpi& H, int row, int count_, int first, int col) : ids(H.ids + row), rows(H.rows), at(0), count(count_) {
+    if (H.top_k == 1) {                         // `first`: the row's first id, if it has one
+      at = count > 0 && first < col;
+      next = at < count ? first : NONE;
+      return;
+    }
     for (int end = count; at < end;) {
       const int mid = (at + end) / 2;
       if (ids[mid * rows] < col) at = mid + 1;
@@ -72,18 +78,27 @@ struct Row {
   float g, gs, k;
   __device__ __forceinline__ Row() : row(0), count(0), live(false), g(0.f), gs(0.f), k(0.f) {}
   __device__ __forceinline__ Row(const HeadEpi& H, int m, int col, int seq, int t_pad) : g(0.f), gs(0.f), k(0.f) {
-    live = m < __ldcg(H.n);
+    const int n = __ldcg(H.n), at = H.row_of[min((long long)m, H.rows - 1)];
+    live = m < n;
     // (bounded by what the buffers were made for: both lie in the caller's memory)
-    row = live ? (int)min((uint32_t)H.row_of[m], (uint32_t)H.rows - 1u) : 0;
-    count = live ? min(H.count[row], H.top_k) : 0;
-    e = Entries(H, row, count, col);
-    if (GRAD && count > 0) {
+    row = live ? (int)min((uint32_t)at, (uint32_t)H.rows - 1u) : 0;
+    const int entries = H.count[row], first = H.ids[row];
+    float scale = H.inv_tau, sum = 1.f;
+    if (GRAD) {
       const int b = row / t_pad, t = row - b * t_pad;
-      g = H.dloss ? H.dloss[(long long)b * seq + t] * H.inv_tau : H.over ? H.inv_tau / fmaxf(*H.over, 1.f) : 1.f;
+      if (H.dloss) scale *= t < seq ? H.dloss[(long long)b * seq + t] : 0.f;
+      else scale = H.over ? scale / fmaxf(*H.over, 1.f) : 1.f;
       k = H.k[row];
-      gs = g / H.sum[row];
-    } else if (GRAD && count < 0) {
-      gs = __int_as_float(0x7fffffff);
+      sum = H.sum[row];
+    }
+    count = live ? min(entries, H.top_k) : 0;
+    e = Entries(H, row, count, first, col);
+    if (GRAD && count > 0) {
+      g = scale;
+      gs = g / sum;
+    } else if (GRAD) {
+      k = 0.f;
+      gs = count < 0 ? __int_as_float(0x7fffffff) : 0.f;
     }
   }
 };
@@ -147,41 +162,45 @@ __device__ __forceinline__ void grad64(const HeadEpi& H, Row<true>& R, uint32_t 
 
 }  // namespace headepi
 
-template <int BN, typename Acc, typename Wait>
+// SETS: of four warps, each with its part of the tile's columns; a partial of the statistics is a set's.
+template <int BN, int SETS, typename Acc, typename Wait>
 __device__ __forceinline__ bool head_stats_tile(const HeadEpi& H, int seq, int t_pad, int m0, int n0, int q, Acc acc, Wait wait) {
-  const int m = m0 + q * 32 + threadIdx.x % 32;
-  headepi::Row<false> R(H, m, n0, seq, t_pad);
+  constexpr int WIDTH = BN / SETS;
+  const int m = m0 + q * 32 + threadIdx.x % 32, first = SETS == 1 ? 0 : ((int)threadIdx.x / 32 - 2) / 4 * WIDTH;
+  headepi::Row<false> R(H, m, n0 + first, seq, t_pad);
   if (!wait()) return false;
   tc::tc_fence_after();
   float k = -INFINITY, s = 0.f;
 #pragma unroll 1
-  for (int pn = 0; pn < BN / 64 && n0 + pn * 64 < H.vocab; ++pn) {
+  for (int c = first; c < first + WIDTH && n0 + c < H.vocab; c += 64) {
     uint32_t v[64];
-    headepi::load_panel(acc, pn, v);
-    headepi::stats64(H, R, v, n0 + pn * 64, k, s);
+    headepi::load_panel(acc, c / 64, v);
+    headepi::stats64(H, R, v, n0 + c, k, s);
   }
-  if (R.live) H.part[(long long)R.row * H.tiles + n0 / HEAD_TILE] = make_float2(k, s);
+  if (R.live && n0 + first < H.vocab) H.part[(long long)R.row * H.tiles + (n0 + first) / WIDTH] = make_float2(k, s);
   return true;
 }
 
-template <int BN, typename Problem, typename Acc, typename Wait>
+template <int BN, int SETS, typename Problem, typename Acc, typename Wait>
 __device__ __forceinline__ bool head_grad_tile(const HeadEpi& H, const Problem& P, int m0, int n0, int q, Acc acc, uint32_t stg0, int& pc, Wait wait) {
-  const int lane = threadIdx.x % 32;
-  headepi::Row<true> R(H, m0 + q * 32 + lane, H.col0 + n0, P.seq, P.t_pad);
+  constexpr int WIDTH = BN / SETS;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, first = SETS == 1 ? 0 : (warp - 2) / 4 * WIDTH;
+  headepi::Row<true> R(H, m0 + q * 32 + lane, H.col0 + n0 + first, P.seq, P.t_pad);
   if (!wait()) return false;
   tc::tc_fence_after();
 #pragma unroll 1
-  for (int pn = 0; pn < BN / 64; ++pn) {
-    const int n = n0 + pn * 64;
+  for (int c = first; c < first + WIDTH; c += 64) {
+    const int n = n0 + c;
     if (n >= P.n) break;
     uint32_t v[64];
-    headepi::load_panel(acc, pn, v);
+    headepi::load_panel(acc, c / 64, v);
     headepi::grad64(H, R, v, H.col0 + n);
     uint32_t ow[32];
 #pragma unroll
     for (int j = 0; j < 32; ++j) ow[j] = R.count ? tc::pack_bf16(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])) : 0u;
-    // as in epilogue_tile: the staging tile's store two panels ago has been read
-    const uint32_t stg = stg0 + (uint32_t)(q * 2 + (pc & 1)) * 4096u;
+    // as in epilogue_tile: the staging tile's last store has been read
+    const uint32_t stg = stg0 + (SETS == 2 ? (uint32_t)(warp - 2) : (uint32_t)(q * 2 + (pc & 1))) * 4096u;
+    if (SETS == 2 && lane == 0) tc::bulk_wait_group_read0();
     __syncwarp();
 #pragma unroll
     for (int j = 0; j < 8; ++j) tc::sts4(stg + lane * 128 + (((uint32_t)j ^ (uint32_t)(lane & 7)) * 16), &ow[4 * j]);
@@ -190,7 +209,7 @@ __device__ __forceinline__ bool head_grad_tile(const HeadEpi& H, const Problem& 
     if (lane == 0) {
       tc::tma_store_3d(&P.tc, stg, 0, m0 + q * 32, n / 64);
       tc::bulk_commit_group();
-      tc::bulk_wait_group_read1();
+      if (SETS == 1) tc::bulk_wait_group_read1();
     }
     ++pc;
   }

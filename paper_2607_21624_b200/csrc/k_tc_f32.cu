@@ -197,8 +197,9 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_tc_f32_kernel(const __grid_co
   if constexpr (!HEAD) total_kb = P.total_kb;
   const int area_kb = HEAD ? gemm_slice_begin(total_kb, areas(pi), area) : 0, area_n = HEAD ? gemm_slice_begin(total_kb, areas(pi), area + 1) - area_kb : total_kb;
   const int kb_begin = area_kb + gemm_slice_begin(area_n, G.slices, slice), n_kb = area_kb + gemm_slice_begin(area_n, G.slices, slice + 1) - kb_begin;
-  // a lane of the last eight warps has half a row of the tile, 64 columns
-  static_assert(!SOFTMAX || BN == 128, "half a row is 64 columns");
+  // Softmax: a lane of the last warps has 64 columns of a row of the tile; of BN = 64, four warps have all.  (Few tiles, a step in us with
+  // 128 and 64 columns: 39 tokens of 192 over 3629 columns 46 40, 120 of 768 over 5000 90 81, 200 of 2048 over 2000 146 127.)
+  const bool has_columns = warp >= 10 && (warp - 10) / 4 < BN / 64;
   headepi::Row<EPI == F32_HEAD_GRAD> R;
   const int half_m = m0 + warp % 4 * 32 + lane, half_n = n0 + (warp - 10) / 4 * 64;
   if (warp == 0) {
@@ -326,7 +327,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_tc_f32_kernel(const __grid_co
     for (int i = 0; i < N / 2; ++i) sum[i] = make_float2(0.f, 0.f);
     pdl_wait();
     f32g::group_chores(G, threadIdx.x - 10 * 32, 256);
-    if constexpr (SOFTMAX) R = headepi::Row<EPI == F32_HEAD_GRAD>(G.epi, half_m, G.epi.col0 + half_n, P.seq, P.t_pad);
+    if constexpr (SOFTMAX) { if (has_columns) R = headepi::Row<EPI == F32_HEAD_GRAD>(G.epi, half_m, G.epi.col0 + half_n, P.seq, P.t_pad); }
     for (int it = 0; it < n_kb; ++it) {
       const int b = it & 1;
       if (!tc::mbar_wait(done(b), (it >> 1) & 1, status, 138)) break;
@@ -367,7 +368,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_tc_f32_kernel(const __grid_co
   if (G.slices > 1) tc::cluster_sync_all();
   if (warp == 1) tc::tmem_dealloc(tmem_base, TMEM_COLS);
   if constexpr (SOFTMAX) {
-    if (warp >= 10 && half_n < P.n) {
+    if (has_columns && half_n < P.n) {
       const uint32_t at = base + (uint32_t)((warp % 4 * 32 + lane) * SM::LD + (half_n - n0)) * 4;
       uint32_t v[64];
 #pragma unroll
@@ -405,8 +406,8 @@ Choice choose(const fbl_plan* p, const GemmArgs* gs, const int* order, int count
   double best_t = 1e30;
   for (int bn = 128; bn >= 64; bn -= 64)
     for (int s = 1; s <= 8; s *= 2) {
-      if (gs[0].epi >= 6 && (bn != 128 || s != 1)) continue;
-      if ((p->knob_f32_bn && bn != p->knob_f32_bn && gs[0].epi < 6) || (p->knob_f32_slices && s != p->knob_f32_slices && gs[0].epi < 6)) continue;
+      if (gs[0].epi >= 6 && s != 1) continue;
+      if ((p->knob_f32_bn && bn != p->knob_f32_bn) || (p->knob_f32_slices && s != p->knob_f32_slices && gs[0].epi < 6)) continue;
       constexpr int MAX_SLOTS = 256;
       double end[MAX_SLOTS], cost[f32g::MAX_PROBLEMS], load = 0, whole = 0;      // end: a heap, the earliest on top
       // clusters of 4 and 8 do not fill every group of SMs that shares a scheduler
@@ -508,8 +509,9 @@ cudaError_t launch_gemm_tc_f32_head(const fbl_plan* p, const GemmArgs* gs, int c
         }
         L.G.slices = c.slices;
         L.smem = c.bn == 128 ? Smem<128>::TOTAL : Smem<64>::TOTAL;
-        L.kernel = gs[0].epi == 6 ? gemm_tc_f32_kernel<128, F32_HEAD_STATS> : gs[0].epi == 7 ? gemm_tc_f32_kernel<128, F32_HEAD_GRAD>
-                   : c.bn == 128 ? gemm_tc_f32_kernel<128, F32_HEAD_OUT> : gemm_tc_f32_kernel<64, F32_HEAD_OUT>;
+        L.kernel = gs[0].epi == 6   ? c.bn == 128 ? gemm_tc_f32_kernel<128, F32_HEAD_STATS> : gemm_tc_f32_kernel<64, F32_HEAD_STATS>
+                   : gs[0].epi == 7 ? c.bn == 128 ? gemm_tc_f32_kernel<128, F32_HEAD_GRAD> : gemm_tc_f32_kernel<64, F32_HEAD_GRAD>
+                   : c.bn == 128    ? gemm_tc_f32_kernel<128, F32_HEAD_OUT> : gemm_tc_f32_kernel<64, F32_HEAD_OUT>;
         return cudaFuncSetAttribute(L.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)L.smem);
       },
       [&](HeadLaunch& L) {

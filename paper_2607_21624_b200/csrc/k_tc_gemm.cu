@@ -577,8 +577,8 @@ __device__ __forceinline__ bool epilogue_tile(const TcProblem& P, const HeadProb
 template <int BN, int ESETS, int EPI, typename Acc, typename Wait>
 __device__ __forceinline__ bool any_epilogue_tile(const GroupOf<EPI>& G, const TileCoord& t, int m0, int q, Acc acc, uint32_t stg0, int& pc, Wait wait) {
   const TcProblem& P = G.p[t.prob];
-  if constexpr (EPI == EPI_HEAD_STATS) return head_stats_tile<BN>(G.epi, P.seq, P.t_pad, m0, t.n0, q, acc, wait);
-  else if constexpr (EPI == EPI_HEAD_GRAD) return head_grad_tile<BN>(G.epi, P, m0, t.n0, q, acc, stg0, pc, wait);
+  if constexpr (EPI == EPI_HEAD_STATS) return head_stats_tile<BN, ESETS>(G.epi, P.seq, P.t_pad, m0, t.n0, q, acc, wait);
+  else if constexpr (EPI == EPI_HEAD_GRAD) return head_grad_tile<BN, ESETS>(G.epi, P, m0, t.n0, q, acc, stg0, pc, wait);
   else if constexpr (EPI == EPI_HEAD_OUT) return epilogue_tile<BN, ESETS, EPI>(P, &G.h[t.prob], m0, t.n0, t.slice, q, acc, stg0, pc, wait);
   else return epilogue_tile<BN, ESETS, EPI>(P, nullptr, m0, t.n0, 0, q, acc, stg0, pc, wait);
 }
@@ -1574,7 +1574,34 @@ struct HeadLaunch {
   void (*kernel)(const TcHeadGroup);
 };
 
-// The head's products: 256 columns to a tile where a partial of the softmax statistics is a tile's, on one CTA or a pair; dX beside dW.
+// Tiles of the logits' products: what a set of epilogue warps has of one, `width` columns, is a partial of the softmax statistics.
+// An epilogue takes an exponential a result, and a row's targets and statistics to be looked up, which longer reductions hide.  Clocks
+// from products of 64 columns to reduce (4096 x 32000 outputs, us forward and backward: 93 119, 74 101, 68 87, 93 116, 143 181).
+struct LogitsTile { int kind, sets, width; double epilogue; };
+const LogitsTile LOGITS_TILE[] = {{TILE_PAIR, 1, 256, 5500}, {TILE_WIDE, 1, 256, 5500}, {TILE_WIDE, 2, 128, 4800}, {TILE_NARROW, 2, 64, 3600}, {TILE_SLIM, 1, 64, 2800}};
+constexpr int LOGITS_TILES = sizeof(LOGITS_TILE) / sizeof(LOGITS_TILE[0]);
+
+// The one that is done first.  Where there are few tiles, narrow ones keep more SMs at work on less each (us, forward and backward, 256
+// columns on one CTA -> this choice: 5 tokens of 3392 over 991 columns 20.0 20.9 -> 12.2 14.4, 45 of 576 over 5048 8.2 9.5 -> 5.7 6.5, 3
+// of 704 over 12630 9.4 9.8 -> 7.4 7.8).
+int best_logits_tile(const fbl_plan* p, const TileWork& w, bool stats) {
+  int best = 0;
+  double best_t = 1e300;
+  for (int i = 0; i < LOGITS_TILES; ++i) {
+    const LogitsTile& tile = LOGITS_TILE[i];
+    const bool pair = tile.kind == TILE_PAIR;
+    if (p->knob_gemm_pair >= 0 && (p->knob_gemm_pair == 1) != pair) continue;
+    TileCost c = TILE_COST[tile.kind];
+    c.epilogue = tile.epilogue;
+    double t = tile_makespan(c, &w, 1, pair ? p->sm_count / 2 : p->sm_count);
+    if (stats) t += 1000.0 * ((w.n / tile.width + 255) / 256);            // joining a row's partials, 256 at a time
+    // (the nearly fastest will do if it is pairs, which read W once for 256 rows: 256 tokens of 1024 over 50257 columns 35 -> 30 us a product)
+    if (t < (i > 0 && LOGITS_TILE[best].kind == TILE_PAIR ? 0.95 : 1.0) * best_t) { best_t = t; best = i; }
+  }
+  return best;
+}
+
+// The head's products: logits, or dX beside dW.
 cudaError_t make_head(HeadLaunch& L, const fbl_plan* p, const GemmArgs* gs, int count) {
   TileWork w[2];
   for (int i = 0; i < count; ++i) w[i] = {gs[i].m, gs[i].n, (gs[i].t[0].k + BK - 1) / BK, gs[i].ksplit > 1 ? gs[i].ksplit : 1};
@@ -1583,9 +1610,11 @@ cudaError_t make_head(HeadLaunch& L, const fbl_plan* p, const GemmArgs* gs, int 
   L.order[0] = 0; L.order[1] = 1;
   const int pair_mode = p->knob_gemm_pair;
   if (gs[0].epi) {
-    const double one = tile_makespan(TILE_COST[TILE_WIDE], w, 1, p->sm_count), two = tile_makespan(TILE_COST[TILE_PAIR], w, 1, p->sm_count / 2);
-    // (a tie goes to pairs, which read W once for 256 rows: 256 tokens of 1024 over 50257 columns 35 -> 30 us a product)
-    if (pair_mode >= 0 ? pair_mode == 1 : two < 1.02 * one) kind = TILE_PAIR;
+    const int tile = gs[0].head.tile;
+    if (tile >= LOGITS_TILES || (tile < 0 && gs[0].epi == 6)) return cudaErrorInvalidValue;
+    const LogitsTile& t = LOGITS_TILE[tile >= 0 ? tile : best_logits_tile(p, w[0], gs[0].epi == 6)];
+    kind = t.kind;
+    sets = t.sets;
   } else if (count == 2) {
     // dX's slices and dW's tiles, or the other way round: the longer ones first
     if (w[1].kb / w[1].split > w[0].kb / w[0].split) { std::swap(w[0], w[1]); L.order[0] = 1; L.order[1] = 0; }
@@ -1621,11 +1650,17 @@ cudaError_t make_head(HeadLaunch& L, const fbl_plan* p, const GemmArgs* gs, int 
   const int slots = kind == TILE_PAIR ? p->sm_count / 2 : p->sm_count;
   L.grid = (units < slots ? units : slots) * (kind == TILE_PAIR ? 2 : 1);
   L.threads = sets == 2 ? 320 : 192;
-  L.smem = kind == TILE_PAIR ? (size_t)PairSmem::TOTAL : kind == TILE_WIDE ? (size_t)SmemPlan<256, 4>::TOTAL : (size_t)SmemPlan<128, 6>::TOTAL;
+  L.smem = kind == TILE_PAIR ? (size_t)PairSmem::TOTAL : kind == TILE_WIDE ? (size_t)SmemPlan<256, 4>::TOTAL : kind == TILE_SLIM ? (size_t)SmemPlan<64, 8>::TOTAL : (size_t)SmemPlan<128, 6>::TOTAL;
+  const bool stats = gs[0].epi == 6;
   if (kind == TILE_PAIR)
     L.kernel = gs[0].epi == 6 ? gemm_tc_pair_kernel<EPI_HEAD_STATS> : gs[0].epi == 7 ? gemm_tc_pair_kernel<EPI_HEAD_GRAD> : gemm_tc_pair_kernel<EPI_HEAD_OUT>;
   else if (gs[0].epi)
-    L.kernel = gs[0].epi == 6 ? gemm_tc_kernel<256, 4, 1, EPI_HEAD_STATS> : gemm_tc_kernel<256, 4, 1, EPI_HEAD_GRAD>;
+    switch (kind == TILE_WIDE ? sets : kind == TILE_NARROW ? 3 : 4) {
+      case 1: L.kernel = stats ? gemm_tc_kernel<256, 4, 1, EPI_HEAD_STATS> : gemm_tc_kernel<256, 4, 1, EPI_HEAD_GRAD>; break;
+      case 2: L.kernel = stats ? gemm_tc_kernel<256, 4, 2, EPI_HEAD_STATS> : gemm_tc_kernel<256, 4, 2, EPI_HEAD_GRAD>; break;
+      case 3: L.kernel = stats ? gemm_tc_kernel<128, 6, 2, EPI_HEAD_STATS> : gemm_tc_kernel<128, 6, 2, EPI_HEAD_GRAD>; break;
+      default: L.kernel = stats ? gemm_tc_kernel<64, 8, 1, EPI_HEAD_STATS> : gemm_tc_kernel<64, 8, 1, EPI_HEAD_GRAD>;
+    }
   else if (kind == TILE_WIDE)
     L.kernel = sets == 2 ? gemm_tc_kernel<256, 4, 2, EPI_HEAD_OUT> : gemm_tc_kernel<256, 4, 1, EPI_HEAD_OUT>;
   else
@@ -1648,6 +1683,13 @@ cudaError_t launch_gemm_tc_head(const fbl_plan* p, const GemmArgs* gs, int count
         return point_group(L.G, L.order, gs, status);
       },
       [&](const HeadLaunch& L) { return launch_pdl(L.kernel, dim3(L.grid), dim3(L.threads), L.smem, st, L.G); });
+}
+
+int gemm_tc_logits_tile(const fbl_plan* p, int64_t m, int n, int k, int knob, int* width) {
+  int tile = best_logits_tile(p, {m, n, (k + BK - 1) / BK, 1}, true);
+  if (knob >= 0) tile = std::min(LOGITS_TILES - 1, knob);
+  *width = LOGITS_TILE[tile].width;
+  return tile;
 }
 
 int gemm_tc_choose_own_slices(int sm_count, const GemmShape* dw, const GemmShape& dx) {

@@ -144,6 +144,24 @@ def test_one_block_and_pairs(monkeypatch, pair):
         run_and_compare(cfg(1, 40, 128, 700, tied=tied, top_k=32))
 
 
+@pytest.mark.parametrize("tile", ["0", "1", "2", "3", "4"])
+def test_every_tile_of_the_logits(monkeypatch, tile):
+    """Pairs, one block and one or two sets of epilogue warps; vocabularies that end in every part of a tile."""
+    monkeypatch.setenv("FBL_HEAD_TILE", tile)
+    for vocab in (1, 64, 65, 129, 190, 257, 450):
+        run_and_compare(cfg(2, 75, 192, vocab, tied=vocab % 2 == 0), ignored=0.3)
+    run_and_compare(cfg(3, 130, 64, 3000, tied=True), weighted=True)
+    run_and_compare(cfg(2, 140, 320, 2200, top_k=40, tau=2.0), ignored=0.2)
+
+
+@pytest.mark.parametrize("bn", ["64", "128"])
+def test_fp32_tiles(monkeypatch, bn):
+    monkeypatch.setenv("FBL_F32_BN", bn)
+    for vocab in (1, 33, 64, 65, 97, 129, 450):
+        run_and_compare(cfg(2, 75, 96, vocab, "fp32", tied=vocab % 2 == 0), ignored=0.3)
+    run_and_compare(cfg(2, 140, 320, 2200, "fp32", top_k=40, tau=2.0), weighted=True)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_frozen_sides(dtype):
     c = cfg(2, 77, 128, 1000, dtype)
