@@ -162,11 +162,11 @@ __device__ __forceinline__ void grad64(const HeadEpi& H, Row<true>& R, uint32_t 
 
 }  // namespace headepi
 
-// SETS: of four warps, each with its part of the tile's columns; a partial of the statistics is a set's.
+// SETS: 2: two of four warps, each with half of the tile's columns (a partial of the statistics is a set's); 3: two that take a tile each.
 template <int BN, int SETS, typename Acc, typename Wait>
 __device__ __forceinline__ bool head_stats_tile(const HeadEpi& H, int seq, int t_pad, int m0, int n0, int q, Acc acc, Wait wait) {
-  constexpr int WIDTH = BN / SETS;
-  const int m = m0 + q * 32 + threadIdx.x % 32, first = SETS == 1 ? 0 : ((int)threadIdx.x / 32 - 2) / 4 * WIDTH;
+  constexpr int WIDTH = SETS == 2 ? BN / 2 : BN;
+  const int m = m0 + q * 32 + threadIdx.x % 32, first = SETS != 2 ? 0 : ((int)threadIdx.x / 32 - 2) / 4 * WIDTH;
   headepi::Row<false> R(H, m, n0 + first, seq, t_pad);
   if (!wait()) return false;
   tc::tc_fence_after();
@@ -183,8 +183,8 @@ __device__ __forceinline__ bool head_stats_tile(const HeadEpi& H, int seq, int t
 
 template <int BN, int SETS, typename Problem, typename Acc, typename Wait>
 __device__ __forceinline__ bool head_grad_tile(const HeadEpi& H, const Problem& P, int m0, int n0, int q, Acc acc, uint32_t stg0, int& pc, Wait wait) {
-  constexpr int WIDTH = BN / SETS;
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, first = SETS == 1 ? 0 : (warp - 2) / 4 * WIDTH;
+  constexpr int WIDTH = SETS == 2 ? BN / 2 : BN;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, first = SETS != 2 ? 0 : (warp - 2) / 4 * WIDTH;
   headepi::Row<true> R(H, m0 + q * 32 + lane, H.col0 + n0 + first, P.seq, P.t_pad);
   if (!wait()) return false;
   tc::tc_fence_after();
@@ -199,8 +199,8 @@ __device__ __forceinline__ bool head_grad_tile(const HeadEpi& H, const Problem& 
 #pragma unroll
     for (int j = 0; j < 32; ++j) ow[j] = R.count ? tc::pack_bf16(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])) : 0u;
     // as in epilogue_tile: the staging tile's last store has been read
-    const uint32_t stg = stg0 + (SETS == 2 ? (uint32_t)(warp - 2) : (uint32_t)(q * 2 + (pc & 1))) * 4096u;
-    if (SETS == 2 && lane == 0) tc::bulk_wait_group_read0();
+    const uint32_t stg = stg0 + (SETS >= 2 ? (uint32_t)(warp - 2) : (uint32_t)(q * 2 + (pc & 1))) * 4096u;
+    if (SETS >= 2 && lane == 0) tc::bulk_wait_group_read0();
     __syncwarp();
 #pragma unroll
     for (int j = 0; j < 8; ++j) tc::sts4(stg + lane * 128 + (((uint32_t)j ^ (uint32_t)(lane & 7)) * 16), &ow[4 * j]);

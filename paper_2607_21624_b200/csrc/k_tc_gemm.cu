@@ -587,8 +587,9 @@ __device__ __forceinline__ bool any_epilogue_tile(const GroupOf<EPI>& G, const T
 // shared-memory ring by TMA, warp 1 issues the MMAs into one of two TMEM accumulators, warps 2-5 drain the
 // other accumulator (bias, residual, padding-row mask, bf16 rows in R-Tile order), so the epilogue of
 // one tile overlaps the main loop of the next.
+// ESETS = 3 (the head's): two sets, which take whole tiles in turn, where epilogues are what tiles wait for.
 template <int BN, int STAGES, int ESETS, int EPI>
-__global__ void __maxnreg__(ESETS == 2 ? 168 : EPI == EPI_ACT ? 255 : 224) gemm_tc_kernel(const __grid_constant__ GroupOf<EPI> G) {
+__global__ void __maxnreg__(ESETS >= 2 ? 168 : EPI == EPI_ACT ? 255 : 224) gemm_tc_kernel(const __grid_constant__ GroupOf<EPI> G) {
   using SP = SmemPlan<BN, STAGES>;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (tc::smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -609,7 +610,7 @@ __global__ void __maxnreg__(ESETS == 2 ? 168 : EPI == EPI_ACT ? 255 : 224) gemm_
     }
     for (int a = 0; a < 2; ++a) {
       tc::mbar_init(acc_full(a), 1);
-      tc::mbar_init(acc_empty(a), 128 * ESETS);
+      tc::mbar_init(acc_empty(a), ESETS == 2 ? 256 : 128);
     }
     tc::fence_barrier_init();
   }
@@ -727,13 +728,14 @@ __global__ void __maxnreg__(ESETS == 2 ? 168 : EPI == EPI_ACT ? 255 : 224) gemm_
   } else if (warp >= 2) {
     // ---- epilogue warps ---------------------------------------------------------------------------
     pdl_wait();                                       // the previous kernel may still be reading what we overwrite
-    group_chores(G, threadIdx.x - 64, 128 * ESETS);
+    group_chores(G, threadIdx.x - 64, ESETS == 1 ? 128 : 256);
     const int q = warp % 4;                           // the TMEM lane quarter this warp may access
     int ti = 0, pc = 0;                               // tiles and panels done by this warp
     bool ok = true;
     TileCoord tcd;
     for (Walk<BN, IS_HEAD<EPI>> walk(G); ok && walk.at(G, &tcd); walk.step(), ++ti) {
       const int ab = ti & 1;
+      if (ESETS == 3 && ab != (warp - 2) / 4) continue;
       const bool ready = any_epilogue_tile<BN, ESETS, EPI>(G, tcd, tcd.m0, q, TmemAcc{tmem_base + ((uint32_t)(q * 32) << 16) + ab * BN}, base + SP::STG_OFF, pc, [&] {
         return tc::mbar_wait(acc_full(ab), (ti >> 1) & 1, status, 103);
       });
@@ -766,8 +768,9 @@ struct PairSmem {
   static constexpr uint32_t TOTAL = BAR_OFF + 8 * N_BARS + 16 + 1024;
 };
 
-template <int EPI>
-__global__ void __cluster_dims__(2, 1, 1) __maxnreg__(EPI == EPI_ACT ? 255 : 224) gemm_tc_pair_kernel(const __grid_constant__ GroupOf<EPI> G) {
+// SETS: of epilogue warps, 1 or (the head's logits) 3 as ESETS above.
+template <int EPI, int SETS = 1>
+__global__ void __cluster_dims__(2, 1, 1) __maxnreg__(SETS == 3 ? 168 : EPI == EPI_ACT ? 255 : 224) gemm_tc_pair_kernel(const __grid_constant__ GroupOf<EPI> G) {
   using SP = PairSmem;
   constexpr int STAGES = PAIR_STAGES, BN = PAIR_BN;
   extern __shared__ uint8_t smem_raw[];
@@ -879,15 +882,16 @@ __global__ void __cluster_dims__(2, 1, 1) __maxnreg__(EPI == EPI_ACT ? 255 : 224
   } else if (warp >= 2) {
     // ---- epilogue (both CTAs): this CTA's 128 accumulator rows, as in the single-CTA kernel -------------
     pdl_wait();
-    group_chores(G, threadIdx.x - 64, 128);
+    group_chores(G, threadIdx.x - 64, SETS == 3 ? 256 : 128);
     const int q = warp % 4;
     int ti = 0, pc = 0;
     bool ok = true;
     TileCoord tcd;
     for (PairWalk<IS_HEAD<EPI>> walk(G); ok && walk.at(G, &tcd); walk.step(), ++ti) {
       const int ab = ti & 1;
+      if (SETS == 3 && ab != (warp - 2) / 4) continue;
       const int m0 = tcd.m0 + (int)rank * 128;
-      const bool ready = any_epilogue_tile<BN, 1, EPI>(G, tcd, m0, q, TmemAcc{tmem_base + ((uint32_t)(q * 32) << 16) + ab * BN}, base + SP::STG_OFF, pc, [&] {
+      const bool ready = any_epilogue_tile<BN, SETS, EPI>(G, tcd, m0, q, TmemAcc{tmem_base + ((uint32_t)(q * 32) << 16) + ab * BN}, base + SP::STG_OFF, pc, [&] {
         return tc::mbar_wait(acc_full(ab), (ti >> 1) & 1, status, 113);
       });
       if (!ready) { ok = false; break; }
@@ -1575,10 +1579,13 @@ struct HeadLaunch {
 };
 
 // Tiles of the logits' products: what a set of epilogue warps has of one, `width` columns, is a partial of the softmax statistics.
-// An epilogue takes an exponential a result, and a row's targets and statistics to be looked up, which longer reductions hide.  Clocks
-// from products of 64 columns to reduce (4096 x 32000 outputs, us forward and backward: 93 119, 74 101, 68 87, 93 116, 143 181).
-struct LogitsTile { int kind, sets, width; double epilogue; };
-const LogitsTile LOGITS_TILE[] = {{TILE_PAIR, 1, 256, 5500}, {TILE_WIDE, 1, 256, 5500}, {TILE_WIDE, 2, 128, 4800}, {TILE_NARROW, 2, 64, 3600}, {TILE_SLIM, 1, 64, 2800}};
+// An epilogue is an exponential a result and looking up a row's targets and statistics, which longer reductions hide: `epilogue` are a
+// tile's clocks where nothing else takes as long, `tail` those of the last.  Two sets that take tiles in turn (3) bring the exponential unit
+// nearer to its rate than one did (4096 x 32000 outputs of 64 columns, us forward and backward: one CTA 74 101 -> 57 72, pairs 93 119 -> 68 87;
+// 2048 x 768 over 50257 columns 79 97 -> 77 91).
+struct LogitsTile { int kind, sets, width; double epilogue, tail; };
+const LogitsTile LOGITS_TILE[] = {{TILE_PAIR, 3, 256, 5500, 4500}, {TILE_WIDE, 3, 256, 3200, 4500}, {TILE_WIDE, 2, 128, 4800, 2600}, {TILE_NARROW, 2, 64, 3600, 1500},
+                                  {TILE_SLIM, 1, 64, 2800, 1300}};
 constexpr int LOGITS_TILES = sizeof(LOGITS_TILE) / sizeof(LOGITS_TILE[0]);
 
 // The one that is done first.  Where there are few tiles, narrow ones keep more SMs at work on less each (us, forward and backward, 256
@@ -1592,11 +1599,15 @@ int best_logits_tile(const fbl_plan* p, const TileWork& w, bool stats) {
     const bool pair = tile.kind == TILE_PAIR;
     if (p->knob_gemm_pair >= 0 && (p->knob_gemm_pair == 1) != pair) continue;
     TileCost c = TILE_COST[tile.kind];
+    const int slots = pair ? p->sm_count / 2 : p->sm_count;
+    const long long units = (w.m + c.m - 1) / c.m * ((w.n + c.n - 1) / c.n);
+    if (tile.kind == TILE_WIDE && tile.sets == 2 && units > slots) continue;           // halves of a tile pay where a block has one
     c.epilogue = tile.epilogue;
-    double t = tile_makespan(c, &w, 1, pair ? p->sm_count / 2 : p->sm_count);
-    if (stats) t += 1000.0 * ((w.n / tile.width + 255) / 256);            // joining a row's partials, 256 at a time
-    // (the nearly fastest will do if it is pairs, which read W once for 256 rows: 256 tokens of 1024 over 50257 columns 35 -> 30 us a product)
-    if (t < (i > 0 && LOGITS_TILE[best].kind == TILE_PAIR ? 0.95 : 1.0) * best_t) { best_t = t; best = i; }
+    c.fixed += tile.tail - (units <= slots ? 0.5 : 1.0) * tile.epilogue;
+    double t = tile_makespan(c, &w, 1, slots);
+    if (stats) t += 2500.0 * ((w.n / tile.width + 255) / 256);            // joining a row's partials, 256 at a time
+    // (the nearly fastest will do if it is pairs, which read W once for 256 rows: 256 tokens of 1024 over 50257 columns 33 -> 30 us a product)
+    if (t < (i > 0 && LOGITS_TILE[best].kind == TILE_PAIR ? 0.97 : 1.0) * best_t) { best_t = t; best = i; }
   }
   return best;
 }
@@ -1649,16 +1660,16 @@ cudaError_t make_head(HeadLaunch& L, const fbl_plan* p, const GemmArgs* gs, int 
   if (balanced) { L.G.kb_clocks = (float)c.kb; L.G.unit_clocks = (float)c.unit; L.G.floor_clocks = (float)(two ? 0.5 * c.epilogue : c.epilogue); }
   const int slots = kind == TILE_PAIR ? p->sm_count / 2 : p->sm_count;
   L.grid = (units < slots ? units : slots) * (kind == TILE_PAIR ? 2 : 1);
-  L.threads = sets == 2 ? 320 : 192;
+  L.threads = sets >= 2 ? 320 : 192;
   L.smem = kind == TILE_PAIR ? (size_t)PairSmem::TOTAL : kind == TILE_WIDE ? (size_t)SmemPlan<256, 4>::TOTAL : kind == TILE_SLIM ? (size_t)SmemPlan<64, 8>::TOTAL : (size_t)SmemPlan<128, 6>::TOTAL;
   const bool stats = gs[0].epi == 6;
   if (kind == TILE_PAIR)
-    L.kernel = gs[0].epi == 6 ? gemm_tc_pair_kernel<EPI_HEAD_STATS> : gs[0].epi == 7 ? gemm_tc_pair_kernel<EPI_HEAD_GRAD> : gemm_tc_pair_kernel<EPI_HEAD_OUT>;
+    L.kernel = gs[0].epi == 6 ? gemm_tc_pair_kernel<EPI_HEAD_STATS, 3> : gs[0].epi == 7 ? gemm_tc_pair_kernel<EPI_HEAD_GRAD, 3> : gemm_tc_pair_kernel<EPI_HEAD_OUT>;
   else if (gs[0].epi)
-    switch (kind == TILE_WIDE ? sets : kind == TILE_NARROW ? 3 : 4) {
-      case 1: L.kernel = stats ? gemm_tc_kernel<256, 4, 1, EPI_HEAD_STATS> : gemm_tc_kernel<256, 4, 1, EPI_HEAD_GRAD>; break;
+    switch (kind == TILE_WIDE ? sets : kind == TILE_NARROW ? 4 : 5) {
       case 2: L.kernel = stats ? gemm_tc_kernel<256, 4, 2, EPI_HEAD_STATS> : gemm_tc_kernel<256, 4, 2, EPI_HEAD_GRAD>; break;
-      case 3: L.kernel = stats ? gemm_tc_kernel<128, 6, 2, EPI_HEAD_STATS> : gemm_tc_kernel<128, 6, 2, EPI_HEAD_GRAD>; break;
+      case 3: L.kernel = stats ? gemm_tc_kernel<256, 4, 3, EPI_HEAD_STATS> : gemm_tc_kernel<256, 4, 3, EPI_HEAD_GRAD>; break;
+      case 4: L.kernel = stats ? gemm_tc_kernel<128, 6, 2, EPI_HEAD_STATS> : gemm_tc_kernel<128, 6, 2, EPI_HEAD_GRAD>; break;
       default: L.kernel = stats ? gemm_tc_kernel<64, 8, 1, EPI_HEAD_STATS> : gemm_tc_kernel<64, 8, 1, EPI_HEAD_GRAD>;
     }
   else if (kind == TILE_WIDE)

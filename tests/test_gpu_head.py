@@ -146,7 +146,7 @@ def test_one_block_and_pairs(monkeypatch, pair):
 
 @pytest.mark.parametrize("tile", ["0", "1", "2", "3", "4"])
 def test_every_tile_of_the_logits(monkeypatch, tile):
-    """Pairs, one block and one or two sets of epilogue warps; vocabularies that end in every part of a tile."""
+    """Pairs and one block, sets of epilogue warps in turn, side by side and one; vocabularies that end in every part of a tile."""
     monkeypatch.setenv("FBL_HEAD_TILE", tile)
     for vocab in (1, 64, 65, 129, 190, 257, 450):
         run_and_compare(cfg(2, 75, 192, vocab, tied=vocab % 2 == 0), ignored=0.3)
