@@ -310,20 +310,20 @@ struct TmemAcc {
 // them (this lane's row); `wait`: waits until they are complete (what does not depend on them is requested first).
 // ESETS = 2 (launches in which every block has a single tile, so that nothing overlaps its epilogue): two sets of four
 // warps share the tile's 64-column panels, first and second half, and the epilogue takes half as long.  Each warp then
-// has one staging tile instead of two (the staging area is the same size).
+// has one staging tile instead of two (the staging area is the same size).  ESETS = 3: gemm_tc_kernel.
 // EPI: what the instantiation can fuse besides bias, residual and the row reduction.
 template <int BN, int ESETS, int EPI, typename Acc, typename Wait>
 __device__ __forceinline__ bool epilogue_tile(const TcProblem& P, const HeadProblem* H, int m0, int n0, int slice, int q, Acc acc, uint32_t stg0, int& pc, Wait wait) {
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, set = (warp - 2) / 4;
-  constexpr int PPS = BN / 64 / ESETS;              // panels per set
+  constexpr int PPS = BN / 64 / (ESETS == 2 ? 2 : 1);              // panels per set
   const int row = m0 + q * 32 + lane;               // row of the problem owned by this thread
   const bool pad = P.t_pad > 0 && (row % P.t_pad) >= P.seq;
   const bool has_res = P.residual && row < P.m;
   // a head of the fused row reduction must stay within one warp: where it spans more panels than a set has, the first set
   // takes the whole tile
   const bool whole = ESETS == 2 && P.dot_with && P.dot_hd > 64 * PPS;
-  const int pn_begin = set == 0 ? 0 : (whole ? BN / 64 : PPS);
-  const int pn_end = ESETS == 1 ? BN / 64 : (set == 0 ? (whole ? BN / 64 : PPS) : BN / 64);
+  const int pn_begin = ESETS == 3 || set == 0 ? 0 : (whole ? BN / 64 : PPS);
+  const int pn_end = ESETS != 2 ? BN / 64 : (set == 0 ? (whole ? BN / 64 : PPS) : BN / 64);
   uint4 rv[8];                                    // residual values of the next panel, requested a panel ahead
   if (has_res && pn_begin < pn_end && n0 + pn_begin * 64 < P.n) {
     const __nv_bfloat16* rp = P.residual + ((long long)(n0 / 64 + pn_begin) * P.c_rpad + row) * 64;
@@ -367,8 +367,8 @@ __device__ __forceinline__ bool epilogue_tile(const TcProblem& P, const HeadProb
       // buffer by bulk tensor reductions, or stored there (same staging tiles and swizzle as the bf16 rows below)
 #pragma unroll 1
       for (int hf = 0; hf < 2; ++hf) {
-        const uint32_t stg = stg0 + (ESETS == 2 ? (uint32_t)(warp - 2) : (uint32_t)(q * 2 + (pc & 1))) * 4096u;
-        if (ESETS == 2 && lane == 0) tc::bulk_wait_group_read0();     // the single staging tile's previous contents have been read
+        const uint32_t stg = stg0 + (ESETS >= 2 ? (uint32_t)(warp - 2) : (uint32_t)(q * 2 + (pc & 1))) * 4096u;
+        if (ESETS >= 2 && lane == 0) tc::bulk_wait_group_read0();     // the single staging tile's previous contents have been read
         __syncwarp();
 #pragma unroll
         for (int j = 0; j < 8; ++j)
@@ -459,8 +459,8 @@ __device__ __forceinline__ bool epilogue_tile(const TcProblem& P, const HeadProb
 #pragma unroll 1
         for (int oi = 0; oi < n_out; ++oi) {
           const uint4* ov = oi ? o2 : o1;
-          const uint32_t stg = stg0 + (ESETS == 2 ? (uint32_t)(warp - 2) : (uint32_t)(q * 2 + (pc & 1))) * 4096u;
-          if (ESETS == 2 && lane == 0) tc::bulk_wait_group_read0();
+          const uint32_t stg = stg0 + (ESETS >= 2 ? (uint32_t)(warp - 2) : (uint32_t)(q * 2 + (pc & 1))) * 4096u;
+          if (ESETS >= 2 && lane == 0) tc::bulk_wait_group_read0();
           __syncwarp();
 #pragma unroll
           for (int j = 0; j < 8; ++j)
@@ -554,8 +554,8 @@ __device__ __forceinline__ bool epilogue_tile(const TcProblem& P, const HeadProb
     }
     // Staging tile (pc & 1) of this warp: its previous store (two panels ago) has been read, since lane 0
     // waited for that after committing the store of the panel before this one.
-    const uint32_t stg = stg0 + (ESETS == 2 ? (uint32_t)(warp - 2) : (uint32_t)(q * 2 + (pc & 1))) * 4096u;
-    if (ESETS == 2 && lane == 0) tc::bulk_wait_group_read0();    // one staging tile: the store before has read it
+    const uint32_t stg = stg0 + (ESETS >= 2 ? (uint32_t)(warp - 2) : (uint32_t)(q * 2 + (pc & 1))) * 4096u;
+    if (ESETS >= 2 && lane == 0) tc::bulk_wait_group_read0();    // one staging tile: the store before has read it
     __syncwarp();
 #pragma unroll
     for (int j = 0; j < 8; ++j)
@@ -1645,8 +1645,8 @@ cudaError_t make_head(HeadLaunch& L, const fbl_plan* p, const GemmArgs* gs, int 
   memset(static_cast<void*>(&L.G), 0, sizeof(L.G));
   cudaError_t e = fill_group(L.G, sorted, count, kind == TILE_PAIR ? 128 : c.n, c.m, c.n, &units);
   if (e != cudaSuccess) return e;
-  const bool two = !gs[0].epi && kind != TILE_PAIR && (balanced ? two_sets_pay(c, w[1]) : units <= p->sm_count);
-  if (two || (!gs[0].epi && kind != TILE_PAIR && units <= p->sm_count)) sets = 2;
+  // dX and dW: halves of a tile where a block has one, else tiles in turn (50 tokens of 768 over 50257 columns 35 -> 32 us, one set 37)
+  if (!gs[0].epi && kind != TILE_PAIR) sets = units <= p->sm_count ? 2 : kind == TILE_WIDE ? 3 : two_sets_pay(c, w[count - 1]) ? 2 : 1;
   for (int i = 0; i < count; ++i) {
     const GemmArgs& g = sorted[i];
     HeadProblem& H = L.G.h[i];
@@ -1657,7 +1657,7 @@ cudaError_t make_head(HeadLaunch& L, const fbl_plan* p, const GemmArgs* gs, int 
     H.sums = g.acc_mode;
     H.slice_panels = g.n / 64;
   }
-  if (balanced) { L.G.kb_clocks = (float)c.kb; L.G.unit_clocks = (float)c.unit; L.G.floor_clocks = (float)(two ? 0.5 * c.epilogue : c.epilogue); }
+  if (balanced) { L.G.kb_clocks = (float)c.kb; L.G.unit_clocks = (float)c.unit; L.G.floor_clocks = (float)(sets > 1 ? 0.5 * c.epilogue : c.epilogue); }
   const int slots = kind == TILE_PAIR ? p->sm_count / 2 : p->sm_count;
   L.grid = (units < slots ? units : slots) * (kind == TILE_PAIR ? 2 : 1);
   L.threads = sets >= 2 ? 320 : 192;
@@ -1673,7 +1673,7 @@ cudaError_t make_head(HeadLaunch& L, const fbl_plan* p, const GemmArgs* gs, int 
       default: L.kernel = stats ? gemm_tc_kernel<64, 8, 1, EPI_HEAD_STATS> : gemm_tc_kernel<64, 8, 1, EPI_HEAD_GRAD>;
     }
   else if (kind == TILE_WIDE)
-    L.kernel = sets == 2 ? gemm_tc_kernel<256, 4, 2, EPI_HEAD_OUT> : gemm_tc_kernel<256, 4, 1, EPI_HEAD_OUT>;
+    L.kernel = sets == 3 ? gemm_tc_kernel<256, 4, 3, EPI_HEAD_OUT> : gemm_tc_kernel<256, 4, 2, EPI_HEAD_OUT>;
   else
     L.kernel = sets == 2 ? gemm_tc_kernel<128, 6, 2, EPI_HEAD_OUT> : gemm_tc_kernel<128, 6, 1, EPI_HEAD_OUT>;
   return cudaFuncSetAttribute(L.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)L.smem);
