@@ -18,6 +18,60 @@ __device__ __forceinline__ void start_pass(int32_t* status) {
   if (blockIdx.x == 0 && threadIdx.x == 0) status[0] = status[FBL_EARLY_COLSUM] = status[FBL_EARLY_ROUND] = status[HEAD_TICKET] = 0;
 }
 
+// A block forms an entry's product again, of bf16 values exactly and summed in 64 bits.  The tensor core's own sums are off by some 2^-23
+// of themselves, either way, which over many tokens averages out and of a few is what their losses are off by (one token of 2048, loss
+// 3.9: 1.9e-6, and 2e-7 with this).  It hides beside the rows' copies: a thread's loads are all on their way at once (a warp for an entry,
+// 5 tokens of 3392 with weights by columns: 8 us more).
+template <bool TARGETS>
+__device__ __forceinline__ void exact_products(const HeadExact& E, const int32_t* __restrict__ targets, const HeadRows& R, int seq, int t_pad, int vocab,
+                                               const uint4* __restrict__ X, int first, int step) {
+  constexpr int U = 2;
+  __shared__ double s_sum[8];
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  for (int64_t i = first; i < R.rows * E.top_k; i += step) {
+    const int row = (int)(i % R.rows), e = (int)(i / R.rows), b = row / t_pad, t = row - b * t_pad;
+    const int id = TARGETS ? (t < seq ? targets[b * seq + t] : -1) : e < R.count[row] ? R.ids[i] : -1;
+    if (id < 0 || id >= vocab) continue;       // the block's threads alike
+    const __nv_bfloat16* W = (const __nv_bfloat16*)E.W;
+    double sum = 0.0;
+    for (int v0 = threadIdx.x; v0 < E.d_model / 8; v0 += 256 * U) {
+      uint4 x[U];
+      __align__(16) __nv_bfloat16 w[U][8];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int v = v0 + 256 * u;
+        x[u] = make_uint4(0u, 0u, 0u, 0u);
+        *reinterpret_cast<uint4*>(w[u]) = x[u];
+        if (v >= E.d_model / 8) continue;
+        x[u] = X[((int64_t)(v / 8) * R.rows + row) * 8 + v % 8];
+        if (E.vocab_rows) {
+          *reinterpret_cast<uint4*>(w[u]) = *reinterpret_cast<const uint4*>(W + ((int64_t)(v / 8) * E.w_rows + id) * 64 + v % 8 * 8);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) w[u][k] = W[((int64_t)(id / 64) * E.w_rows + v * 8 + k) * 64 + id % 64];
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const __nv_bfloat16* xs = reinterpret_cast<const __nv_bfloat16*>(&x[u]);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum = fma((double)__bfloat162float(xs[k]), (double)__bfloat162float(w[u][k]), sum);
+      }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0) s_sum[warp] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      double all = 0.0;
+#pragma unroll
+      for (int w = 0; w < 8; ++w) all += s_sum[w];
+      E.z[i] = all;
+    }
+    __syncthreads();
+  }
+}
+
 // Rows of tokens with a loss are brought together, so that the products behind spend nothing on the others (prompts and padding
 // are a fifth to a half of a fine-tuning batch), and what those rows hold does not matter.  A block has `per` rows from its first on
 // and eight column panels of X: it counts the tokens with a loss in front of them, then gives its own their positions and copies
@@ -28,10 +82,15 @@ __device__ __forceinline__ void start_pass(int32_t* status) {
 constexpr int ROWS_PANELS = 8;
 template <bool TARGETS>
 __global__ void __launch_bounds__(256) head_rows_kernel(const int32_t* __restrict__ targets, HeadRows R, int seq, int t_pad, int vocab, int per,
-                                                        const uint4* __restrict__ X, uint4* __restrict__ Xc, int all_panels, int32_t* status) {
+                                                        const uint4* __restrict__ X, uint4* __restrict__ Xc, int all_panels, const HeadExact exact, int32_t* status) {
   __shared__ int s_before[8], s_pos[32], s_count;
   pdl_launch_dependents();
   pdl_wait();
+  const int groups = (all_panels + ROWS_PANELS - 1) / ROWS_PANELS;
+  if ((int)blockIdx.y >= groups) {             // the blocks behind those that copy
+    exact_products<TARGETS>(exact, targets, R, seq, t_pad, vocab, X, (blockIdx.y - groups) * gridDim.x + blockIdx.x, (gridDim.y - groups) * gridDim.x);
+    return;
+  }
   const bool lead = blockIdx.y == 0;
   if (TARGETS && lead) start_pass(status);
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, r = threadIdx.x / 8, vec = threadIdx.x % 8;
@@ -230,7 +289,7 @@ __device__ __forceinline__ float scaled(float k, float s, float top, float c) { 
 constexpr int COMBINE_FEW = 64;
 __global__ void __launch_bounds__(1024) head_combine_kernel(const float2* __restrict__ part, int tiles, const float* __restrict__ z_at,
                                                             HeadRows R, float scale, float* __restrict__ loss, float* __restrict__ total,
-                                                            float2* __restrict__ block_sums, int seq, int t_pad, int32_t* status) {
+                                                            float2* __restrict__ block_sums, int seq, int t_pad, const HeadExact exact, int32_t* status) {
   constexpr int U = 8;
   __shared__ double s_sum[32], s_count[32];
   __shared__ int s_last;
@@ -250,6 +309,7 @@ __global__ void __launch_bounds__(1024) head_combine_kernel(const float2* __rest
     };
     load(0);
     const float y0 = R.y[row], z0 = __ldcg(z_at + row), constant = R.constant[row];      // entry 0, which lane 0 takes
+    const double x0 = exact.z ? __ldcg(exact.z + row) : 0.0;
     const int count = R.count[row];
     float l = 0.f;
     if (count != 0) {
@@ -274,14 +334,28 @@ __global__ void __launch_bounds__(1024) head_combine_kernel(const float2* __rest
       k = top;
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-      float toward = 0.f;                   // sum of y c (k - z)
+      float toward = 0.f, more = 0.f;       // sum of y c (k - z); what s lacks, or has too much of, at the targets
       for (int e = lane; e < count; e += 32) {
         const float y = e ? R.y[(int64_t)e * R.rows + row] : y0, z = e ? __ldcg(z_at + (int64_t)e * R.rows + row) : z0;
         if (y != 0.f) toward = fmaf(y, (k - z) * scale, toward);
+        if (exact.z) {
+          const double x = e ? __ldcg(exact.z + (int64_t)e * R.rows + row) : x0;
+          const float off = (float)(x * exact.unlift - (double)z) * scale;
+          if (fabsf(off) < 1.f) {           // (of infinities, none)
+            toward = fmaf(-y, off, toward);
+            more = fmaf(exp2f((z - k) * scale), expm1f(LN2 * off), more);
+          }
+        }
       }
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) toward += __shfl_xor_sync(0xffffffffu, toward, o);
-      l = count < 0 ? NAN : fmaf(LN2, toward, logf(s)) + constant;
+      l = fmaf(LN2, toward, logf(s)) + constant;
+      if (exact.z) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) more += __shfl_xor_sync(0xffffffffu, more, o);
+        l += log1pf(more / s);
+      }
+      if (count < 0) l = NAN;
       if (lane == 0) { R.k[row] = k; R.sum[row] = s; }
       sum += l;
       counted += 1.0;
@@ -405,12 +479,13 @@ cudaError_t launch_pack_columns(int dtype, int unpack, const void* src, void* ds
   return unpack ? go(pack_columns_kernel<__nv_bfloat16, false>, (__nv_bfloat16*)0) : go(pack_columns_kernel<__nv_bfloat16, true>, (__nv_bfloat16*)0);
 }
 cudaError_t launch_head_rows(int dtype, const int32_t* targets, const HeadRows& R, int seq, int t_pad, int vocab, const void* X, int d_model,
-                             int32_t* status, cudaStream_t st) {
+                             const HeadExact& exact, int32_t* status, cudaStream_t st) {
   const int panels = d_model / (dtype == FBL_DTYPE_FP32 ? 32 : 64);
   const int64_t per = R.rows <= 32 * 1024 ? 32 : (R.rows / 1024 + 31) / 32 * 32;
-  const dim3 grid((unsigned)((R.rows + per - 1) / per), (unsigned)((panels + ROWS_PANELS - 1) / ROWS_PANELS));
+  dim3 grid((unsigned)((R.rows + per - 1) / per), (unsigned)((panels + ROWS_PANELS - 1) / ROWS_PANELS));
+  if (exact.z) grid.y += (unsigned)((R.rows * exact.top_k + grid.x - 1) / grid.x);       // a block for each
   return launch_pdl(targets ? head_rows_kernel<true> : head_rows_kernel<false>, grid, dim3(256), 0, st,
-                    targets, R, seq, t_pad, vocab, (int)per, (const uint4*)X, (uint4*)R.x, panels, status);
+                    targets, R, seq, t_pad, vocab, (int)per, (const uint4*)X, (uint4*)R.x, panels, exact, status);
 }
 cudaError_t launch_teacher_entries(const int32_t* ids, const float* logits, int top_k, float temperature, const HeadRows& R, int seq, int t_pad,
                                    int vocab, int32_t* status, cudaStream_t st) {
@@ -419,10 +494,10 @@ cudaError_t launch_teacher_entries(const int32_t* ids, const float* logits, int 
                     vocab, status);
 }
 cudaError_t launch_head_combine(const float2* part, int tiles, const float* z_at, const HeadRows& R, float scale, float* loss, float* total,
-                                float* block_sums, int seq, int t_pad, int32_t* status, cudaStream_t st) {
+                                float* block_sums, int seq, int t_pad, const HeadExact& exact, int32_t* status, cudaStream_t st) {
   const bool few = R.rows <= COMBINE_FEW;
-  return launch_pdl(head_combine_kernel, dim3(few ? 1u : (unsigned)(R.rows / 8)), dim3(few ? (unsigned)R.rows / 8 * 128 : 256), 0, st, part, tiles, z_at, R, scale, loss, total, (float2*)block_sums, seq,
-                    t_pad, status);
+  return launch_pdl(head_combine_kernel, dim3(few ? 1u : (unsigned)(R.rows / 8)), dim3(few ? (unsigned)R.rows / 8 * 128 : 256), 0, st, part, tiles, z_at,
+                    R, scale, loss, total, (float2*)block_sums, seq, t_pad, exact, status);
 }
 cudaError_t launch_head_scatter(int dtype, int sm_count, const float* acc, int areas, const HeadRows& R, int d_model, const float* over, float alpha,
                                 void* dX, cudaStream_t st) {

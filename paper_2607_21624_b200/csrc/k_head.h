@@ -17,13 +17,22 @@ struct HeadRows {
   void* x;                    // the products' rows of X, zeros behind them to whole tiles
 };
 
+// Products at the targets formed again in 64 bits by the kernel that brings the rows together (bf16, few of them): z [entry][row] null: not.
+struct HeadExact {
+  double* z;
+  const void* W;
+  int64_t w_rows;
+  int vocab_rows, d_model, top_k;
+  double unlift;              // what the other products come out as, over what they are
+};
+
 // Labels, or what teacher_entries has left in `count`, to positions; the rows of X with a loss to R.x.
 cudaError_t launch_head_rows(int dtype, const int32_t* targets, const HeadRows& R, int seq, int t_pad, int vocab, const void* X, int d_model,
-                             int32_t* status, cudaStream_t st);
+                             const HeadExact& exact, int32_t* status, cudaStream_t st);
 cudaError_t launch_teacher_entries(const int32_t* ids, const float* logits, int top_k, float temperature, const HeadRows& R, int seq, int t_pad,
                                    int vocab, int32_t* status, cudaStream_t st);
 cudaError_t launch_head_combine(const float2* part, int tiles, const float* z_at, const HeadRows& R, float scale, float* loss, float* total,
-                                float* block_sums, int seq, int t_pad, int32_t* status, cudaStream_t st);
+                                float* block_sums, int seq, int t_pad, const HeadExact& exact, int32_t* status, cudaStream_t st);
 // dX from the areas' sums, times alpha / max(*over, 1) where `over` is not null
 cudaError_t launch_head_scatter(int dtype, int sm_count, const float* acc, int areas, const HeadRows& R, int d_model, const float* over, float alpha,
                                 void* dX, cudaStream_t st);

@@ -317,6 +317,33 @@ def test_confident_and_large_logits(dtype, tied):
     compare(c, inp, run, ref)
 
 
+@pytest.mark.parametrize("top_k", [0, 3])
+@pytest.mark.parametrize("tied", [False, True], ids=["dv", "vd"])
+def test_few_tokens_targets_in_64_bits(tied, top_k):
+    """Losses of few tokens take the products at their targets from sums in 64 bits.  A target's logit of 1024 and 4095 terms of 2^-17,
+    which a sum of 24 bits that cuts its additions off loses in part (2^-5 in all, of which 16 columns lose up to 2^-13), beside a rival of
+    1024 exactly: the loss, log(1 + 2^(-2^-5 log2 e)), would be off by up to 2^-6.  What is left is what logits are scaled up by against
+    such cuts, (2.2e-8 + 1e-9 d) 1024 for the rival, which has none: 4.3e-3 of it at most.  (Gradients take the softmax from the sums that
+    are cut off: p may be off by p (1 - p) 2^-6 here, as dz_slack has it, all tokens alike, which their norms' bound does not.)"""
+    d, v, n = 4096, 70, 11
+    c = cfg(1, n, d, v, "bf16", tied, top_k)
+    inp = make_head_inputs(c)
+    w, x = np.zeros((d, v)), np.full((1, n, d), 2.0 ** -9)
+    w[0, 41] = w[0, 66] = x[..., 0] = 32.0
+    w[1:, 66] = 2.0 ** -8
+    inp.update(X=x, W=w.T.copy() if tied else w)
+    if top_k:
+        inp.update(top_ids=np.array([[[-1, 66, -1]] * n], dtype=np.int32), top_logits=np.ones((1, n, 3)))
+    else:
+        inp["targets"] = np.full((1, n), 66, dtype=np.int32)
+    ref = orc.head_fwd_bwd(c, inp)
+    run = HeadRunner(c, guard_bytes=4096)
+    run.load_inputs(inp)
+    run.step()
+    assert (np.abs(run.fetch("loss") - ref["loss"]) <= 4.4e-3).all()
+    assert run.guards_intact() == []
+
+
 @pytest.mark.parametrize("tied", [False, True], ids=["dv", "vd"])
 def test_fp32_operands_beyond_the_parts_range(monkeypatch, tied):
     """Hidden states of 2^100 and weights of 2^97, whose products and gradients leave the range that operands in parts have: their tiles
