@@ -459,8 +459,9 @@ int64_t fbl_norm_launch_count(const fbl_norm_plan* plan);
  * together there; `saved` serves any number of backward calls.  Outputs overlap no input and no workspace (dW is written while W
  * is still read).
  * bf16 storage: products on bf16 operands with fp32 sums; statistics, losses and gradients in fp32, dz rounded to bf16 as an
- * operand of the last two products; of up to 64 padded token rows the logits at the targets enter the losses from sums in
- * 64 bits.  The sums of dX over pieces and slices of the vocabulary are fp32, in a fixed order.
+ * operand of the last two products.  Of up to 64 padded token rows dz comes in two bf16 values, its rounding and the rest, and the
+ * logits at the targets enter the losses from sums in 64 bits.  The sums of dX over pieces and slices of the vocabulary are fp32, in a
+ * fixed order.
  * FBL_HEAD_PIECE, FBL_HEAD_SLICES and FBL_HEAD_TILE, read at plan creation, override the columns of a piece, the slices of dX's
  * reduction and the tile of the bf16 logits' products (for tuning and tests only). */
 typedef struct {

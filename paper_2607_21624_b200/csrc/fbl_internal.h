@@ -115,6 +115,7 @@ struct HeadEpi {
   const float *k, *sum;         // backward: the row's k and sum
   const float *dloss, *over;    // backward: the gradient of each token's loss [batch * seq], or else 1 / max(*over, 1), or else 1
   float inv_tau;
+  int second;                   // backward: products' rows from here on are the first ones again, and get what dz loses by its rounding (0: none)
 };
 struct GemmArgs {
   int m, n, n_terms;

@@ -59,6 +59,10 @@ double logit_lift(int d_model) { return 2.2e-8 + 1.6e-8 * (d_model / 16); }
 // of 2048, where one token's was off by up to 1.2e-6).
 constexpr int EXACT_ROWS = 64, EXACT_ENTRIES = 1024;
 
+// Up to so many rows, half of a tile of 128, dz comes in two parts, the second below the first (head_epilogue.cuh): the rows are there
+// anyway, and what it costs is writing and reading dz twice (us a step, 50 tokens of 768 over 50257 columns 88 -> 90).
+constexpr int SECOND_ROWS = 64;
+
 struct fbl_head_plan {
   fbl_head_desc d;
   fbl_plan* base;
@@ -68,6 +72,8 @@ struct fbl_head_plan {
   int top_k, tiles;             // entries a row; partials of the softmax statistics
   int logits_tile, grad_tile;   // HeadEpi.tile of the two passes
   int piece, pieces, slices;    // columns of a piece; pieces; areas that dX's reduction is cut into
+  int second;                   // few rows: where they lie again, for dz's second part (0: nowhere)
+  int64_t x_rows;               // rows of the products
   float scale;                  // from a product to a logit times log2 e
   size_t sv_ids, sv_y, sv_count, sv_constant, sv_row_of, sv_pos, sv_n, sv_k, sv_sum, sv_total, sv_x, saved_bytes;
   bool exact;                   // products at the targets formed again in 64 bits
@@ -92,7 +98,7 @@ HeadRows rows_of(const fbl_head_plan* p, const void* saved) {
   R.row_of = (int32_t*)(sv + p->sv_row_of); R.pos = (int32_t*)(sv + p->sv_pos); R.n = (int32_t*)(sv + p->sv_n);
   R.k = (float*)(sv + p->sv_k); R.sum = (float*)(sv + p->sv_sum);
   R.total = (float*)(sv + p->sv_total);
-  R.x = sv + p->sv_x;
+  R.x = sv + p->sv_x; R.x_rows = p->x_rows; R.second = p->second;
   return R;
 }
 
@@ -102,6 +108,7 @@ HeadEpi epilogue_of(const fbl_head_plan* p, const HeadRows& R, int col0) {
   h.vocab = p->d.vocab; h.col0 = col0; h.top_k = p->top_k; h.scale = p->scale;
   h.k = R.k; h.sum = R.sum;
   h.inv_tau = 1.f / p->d.temperature;
+  h.second = p->second;
   return h;
 }
 
@@ -119,12 +126,12 @@ int64_t piece_rows(const fbl_head_plan* p, int col0, int cols) {
 // The products behind a piece of dz but for addresses: a token-axis reduction, dz^T X [vocab, d_model] or X^T dz, and dz W^T.
 GemmArgs dw_product(const fbl_head_plan* p, int cols) {
   GemmArgs g = {};
-  const int n = (int)p->n_pad, D = p->d.d_model;
-  g.dyn = 2;
+  const int n = (int)p->x_rows, D = p->d.d_model;
+  g.dyn = p->second ? 0 : 2;
   g.n_terms = 1;
   if (p->d.vocab_rows) { g.m = cols; g.n = D; }
   else { g.m = D; g.n = cols; }
-  g.t[0] = {nullptr, p->n_pad, 1, nullptr, p->n_pad, 0, n, 0};
+  g.t[0] = {nullptr, n, 1, nullptr, n, 0, n, 0};
   g.c_rpad = p->w_rows;
   return g;
 }
@@ -132,9 +139,9 @@ GemmArgs dx_product(const fbl_head_plan* p, int cols) {
   GemmArgs g = {};
   g.dyn = 1;
   g.n_terms = 1;
-  g.m = (int)p->n_pad; g.n = p->d.d_model;
-  g.t[0] = {nullptr, p->n_pad, 0, nullptr, p->w_rows, p->d.vocab_rows ? 0 : 1, cols, 0};
-  g.c_rpad = p->n_pad;
+  g.m = (int)p->x_rows; g.n = p->d.d_model;
+  g.t[0] = {nullptr, p->x_rows, 0, nullptr, p->w_rows, p->d.vocab_rows ? 0 : 1, cols, 0};
+  g.c_rpad = p->x_rows;
   return g;
 }
 
@@ -142,10 +149,10 @@ GemmArgs dx_product(const fbl_head_plan* p, int cols) {
 GemmArgs logits_product(const fbl_head_plan* p, const HeadRows& R, const void* W, int col0, int cols) {
   GemmArgs g = {};
   g.rows = R.n + 1; g.dyn = 1;
-  g.m = (int)p->n_pad; g.n = cols; g.n_terms = 1;
-  g.t[0] = {R.x, p->n_pad, 0, weights_at(p, W, col0), p->w_rows, p->d.vocab_rows, p->d.d_model, piece_rows(p, col0, cols)};
+  g.m = (int)p->x_rows; g.n = cols; g.n_terms = 1;
+  g.t[0] = {R.x, p->x_rows, 0, weights_at(p, W, col0), p->w_rows, p->d.vocab_rows, p->d.d_model, piece_rows(p, col0, cols)};
   g.b_static = 1;
-  g.c_rpad = p->n_pad;
+  g.c_rpad = p->x_rows;
   g.seq = p->d.seq; g.t_pad = p->base->t_pad;
   return g;
 }
@@ -206,12 +213,14 @@ int fbl_head_plan_create(const fbl_head_desc* desc, fbl_head_plan** out) {
   if (!p) { fbl_plan_destroy(base); return FBL_ERR_INVALID_ARG; }
   p->d = d; p->base = base; p->n_pad = base->n_pad; p->launches = 0;
   const bool bf16 = d.dtype == FBL_DTYPE_BF16;
+  p->second = bf16 && p->n_pad <= SECOND_ROWS ? (int)p->n_pad : 0;
+  p->x_rows = p->second ? 2 * p->n_pad : p->n_pad;
   p->cols = (int)up(d.vocab, base->tw);
   p->w_rows = d.vocab_rows ? up(d.vocab, 8) : d.d_model;
   p->top_k = d.top_k ? d.top_k : 1;
   int width = HEAD_TILE_F32;
   p->grad_tile = getenv("FBL_HEAD_TILE") ? atoi(getenv("FBL_HEAD_TILE")) : -1;                                               // tuning / test knob
-  p->logits_tile = bf16 ? gemm_tc_logits_tile(base, p->n_pad, p->cols, d.d_model, p->grad_tile, &width) : 0;
+  p->logits_tile = bf16 ? gemm_tc_logits_tile(base, p->x_rows, p->cols, d.d_model, p->grad_tile, &width) : 0;
   if (p->grad_tile >= 0) p->grad_tile = p->logits_tile;
   p->tiles = (p->cols + width - 1) / width;
   p->scale = (float)(1.4426950408889634 / (double)d.temperature * (1.0 + (bf16 ? logit_lift(d.d_model) : 0.0)));
@@ -254,9 +263,9 @@ int fbl_head_plan_create(const fbl_head_desc* desc, fbl_head_plan** out) {
   p->sv_k = take(o, n * 4);
   p->sv_sum = take(o, n * 4);
   p->sv_total = take(o, 8);
-  p->sv_x = take(o, n * d.d_model * base->e);
+  p->sv_x = take(o, (size_t)p->x_rows * d.d_model * base->e);
   p->saved_bytes = o;
-  const size_t piece_bytes = n * p->piece * base->e;
+  const size_t piece_bytes = (size_t)p->x_rows * p->piece * base->e;
   o = FBL_ALIGN;                // status word
   p->sf_part = take(o, n * p->tiles * sizeof(float2));
   p->sf_z = take(o, n * p->top_k * 4);
@@ -266,7 +275,7 @@ int fbl_head_plan_create(const fbl_head_desc* desc, fbl_head_plan** out) {
   p->scratch_fwd_bytes = o;
   o = FBL_ALIGN;
   p->sb_dz = take(o, piece_bytes);
-  p->sb_acc = take(o, n * d.d_model * 4 * p->slices);
+  p->sb_acc = take(o, (size_t)p->x_rows * d.d_model * 4 * p->slices);
   p->scratch_bwd_bytes = o;
   *out = p;
   return FBL_OK;

@@ -9,7 +9,8 @@
 // k and s are a whole row's by then (head_combine_kernel).  Logits only ever enter as distances from the row's largest: a target that
 // holds all of its row's probability gives log s = log 1 exactly, and logits of any size have a loss.  Sums are fp32; dz is
 // rounded to the storage type, as an operand of the two products that consume it (bf16: half a step of 2^-8 of each value, as
-// large as the rounding of the results).
+// large as the rounding of the results; up to 64 rows, half of a tile, its other half takes what that loses, with the same rows of X, so that
+// the gradients of few tokens are as near as their own rounding: 3.5e-3 of their norm -> 1.7e-3).
 //
 // What bounds a tile's epilogue is the exponential unit: 256 columns of 32 rows a warp, a lane's 256 exponentials at 8 clocks a
 // warp instruction are 2048 clocks, beside some 1200 issued instructions; the products of the next tile take 640 clocks per 64 columns
@@ -74,12 +75,14 @@ template <bool GRAD>
 struct Row {
   Entries e;
   int row, count;
+  bool low;                   // a row's second: what dz loses by its rounding
   bool live;                  // rows behind the last token's are zero: the reduction over tokens ends inside a k-block
   float g, gs, k;
-  __device__ __forceinline__ Row() : row(0), count(0), live(false), g(0.f), gs(0.f), k(0.f) {}
-  __device__ __forceinline__ Row(const HeadEpi& H, int m, int col, int seq, int t_pad) : g(0.f), gs(0.f), k(0.f) {
+  __device__ __forceinline__ Row() : row(0), count(0), low(false), live(false), g(0.f), gs(0.f), k(0.f) {}
+  __device__ __forceinline__ Row(const HeadEpi& H, int m, int col, int seq, int t_pad) : low(H.second && m >= H.second), g(0.f), gs(0.f), k(0.f) {
+    if (low) m -= H.second;
     const int n = __ldcg(H.n), at = H.row_of[min((long long)m, H.rows - 1)];
-    live = m < n;
+    live = m < n && (GRAD || !low);
     // (bounded by what the buffers were made for: both lie in the caller's memory)
     row = live ? (int)min((uint32_t)at, (uint32_t)H.rows - 1u) : 0;
     const int entries = H.count[row], first = H.ids[row];
@@ -195,6 +198,13 @@ __device__ __forceinline__ bool head_grad_tile(const HeadEpi& H, const Problem& 
     uint32_t v[64];
     headepi::load_panel(acc, c / 64, v);
     headepi::grad64(H, R, v, H.col0 + n);
+    if (R.low) {
+#pragma unroll
+      for (int j = 0; j < 64; ++j) {
+        const float f = __uint_as_float(v[j]);
+        v[j] = __float_as_uint(f - __bfloat162float(__float2bfloat16_rn(f)));
+      }
+    }
     uint32_t ow[32];
 #pragma unroll
     for (int j = 0; j < 32; ++j) ow[j] = R.count ? tc::pack_bf16(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])) : 0u;

@@ -97,8 +97,8 @@ __global__ void __launch_bounds__(256) head_rows_kernel(const int32_t* __restric
   const int first = blockIdx.x * per, end = min(first + per, (int)R.rows);
   const int p0 = blockIdx.y * ROWS_PANELS, panels = min(ROWS_PANELS, all_panels - p0);
   const uint4* from = X + (int64_t)p0 * R.rows * 8 + vec;
-  uint4* to = Xc + (int64_t)p0 * R.rows * 8 + vec;
-  const int64_t pitch = R.rows * 8;
+  uint4* to = Xc + (int64_t)p0 * R.x_rows * 8 + vec;
+  const int64_t pitch = R.rows * 8, x_pitch = R.x_rows * 8;
   uint4 x[ROWS_PANELS];
   auto load = [&](int row) {
 #pragma unroll
@@ -154,8 +154,11 @@ __global__ void __launch_bounds__(256) head_rows_kernel(const int32_t* __restric
     const int pos = s_pos[r];
     if (pos >= 0) {
 #pragma unroll
-      for (int p = 0; p < ROWS_PANELS; ++p)
-        if (p < panels) to[p * pitch + (int64_t)pos * 8] = x[p];
+      for (int p = 0; p < ROWS_PANELS; ++p) {
+        if (p >= panels) break;
+        to[p * x_pitch + (int64_t)pos * 8] = x[p];
+        if (R.second) to[p * x_pitch + (int64_t)(pos + R.second) * 8] = x[p];
+      }
     }
     before += s_count;
     if (r0 + 32 < end) load(r0 + 32 + r);
@@ -164,9 +167,12 @@ __global__ void __launch_bounds__(256) head_rows_kernel(const int32_t* __restric
   if (end < (int)R.rows) return;
   // the last rows' blocks: how many there are, and zeros behind them up to a whole tile (a reduction over tokens ends inside a k-block)
   if (lead && threadIdx.x == 0) { R.n[0] = before; R.n[1] = max(before, 1); }
-  const int stop = min((int)R.rows, (max(before, 1) + 127) / 128 * 128);
+  const int stop = R.second ? R.second : min((int)R.x_rows, (max(before, 1) + 127) / 128 * 128);
   for (int c = before + r; c < stop; c += 32)
-    for (int p = 0; p < panels; ++p) to[p * pitch + (int64_t)c * 8] = make_uint4(0u, 0u, 0u, 0u);
+    for (int p = 0; p < panels; ++p) {
+      to[p * x_pitch + (int64_t)c * 8] = make_uint4(0u, 0u, 0u, 0u);
+      if (R.second) to[p * x_pitch + (int64_t)(c + R.second) * 8] = make_uint4(0u, 0u, 0u, 0u);
+    }
 }
 
 // A teacher's top logits: their softmax over the ids given, ids given twice added up, sorted by id.  A warp has a row, a lane every
@@ -408,12 +414,12 @@ __global__ void __launch_bounds__(1024) head_combine_kernel(const float2* __rest
   }
 }
 
-// dX: the areas' sums times alpha / max(*over, 1) where `over` is not null, at the tokens' own rows, and zeros at the rows without a
+// dX: the areas' sums (of a row and its second, where there are such) times alpha / max(*over, 1) where `over` is not null, at the tokens' own rows, and zeros at the rows without a
 // loss.  A warp has 128 consecutive bytes of sums: with GROUPS = 4 its quarters take every fourth area each and are added up in
 // that order (few elements and many areas: 56 x 768 of 24 areas), with 1 four pieces of 128 bytes.  Bound by memory.
-template <typename T, int GROUPS>
-__global__ void __launch_bounds__(256) head_scatter_kernel(const float* __restrict__ acc, int areas, HeadRows R, int64_t n, const float* __restrict__ over,
-                                                           float alpha, T* __restrict__ dX) {
+template <typename T, int GROUPS, bool SECOND>
+__global__ void __launch_bounds__(256) head_scatter_kernel(const float* __restrict__ acc, int areas, int64_t area, HeadRows R, int64_t n,
+                                                           const float* __restrict__ over, float alpha, T* __restrict__ dX) {
   constexpr int TW = tile_w_of<T>::value;
   pdl_launch_dependents();
   pdl_wait();
@@ -427,11 +433,15 @@ __global__ void __launch_bounds__(256) head_scatter_kernel(const float* __restri
     const int pos = R.pos[line - panel * R.rows];
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
     if (pos >= 0 && pos < R.rows) {
-      const float* from = acc + (panel * R.rows + pos) * TW + i % TW;
+      const float* from = acc + (panel * R.x_rows + pos) * TW + i % TW;
 #pragma unroll 8
       for (int k = group; k < areas; k += GROUPS) {
-        const float4 v = __ldcg(reinterpret_cast<const float4*>(from + k * n));
+        const float4 v = __ldcg(reinterpret_cast<const float4*>(from + k * area));
         s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+        if (SECOND) {
+          const float4 u = __ldcg(reinterpret_cast<const float4*>(from + k * area + R.second * TW));
+          s.x += u.x; s.y += u.y; s.z += u.z; s.w += u.w;
+        }
       }
     }
     if (GROUPS > 1) {
@@ -504,7 +514,8 @@ cudaError_t launch_head_scatter(int dtype, int sm_count, const float* acc, int a
   const int64_t n = R.rows * d_model;                        // whole tiles: a multiple of 256 bytes of sums
   const bool spread = areas >= 4 && n <= (int64_t)sm_count * 8 * 1024;
   const dim3 grid((unsigned)min((int64_t)sm_count * 8, (n + (spread ? 255 : 1023)) / (spread ? 256 : 1024)));
-  auto go = [&](auto kernel, auto* t) { return launch_pdl(kernel, grid, dim3(256), 0, st, acc, areas, R, n, over, alpha, t); };
-  if (dtype == FBL_DTYPE_FP32) return spread ? go(head_scatter_kernel<float, 4>, (float*)dX) : go(head_scatter_kernel<float, 1>, (float*)dX);
-  return spread ? go(head_scatter_kernel<__nv_bfloat16, 4>, (__nv_bfloat16*)dX) : go(head_scatter_kernel<__nv_bfloat16, 1>, (__nv_bfloat16*)dX);
+  auto go = [&](auto kernel, auto* t) { return launch_pdl(kernel, grid, dim3(256), 0, st, acc, areas, R.x_rows * d_model, R, n, over, alpha, t); };
+  if (dtype == FBL_DTYPE_FP32) return spread ? go(head_scatter_kernel<float, 4, false>, (float*)dX) : go(head_scatter_kernel<float, 1, false>, (float*)dX);
+  if (R.second) return spread ? go(head_scatter_kernel<__nv_bfloat16, 4, true>, (__nv_bfloat16*)dX) : go(head_scatter_kernel<__nv_bfloat16, 1, true>, (__nv_bfloat16*)dX);
+  return spread ? go(head_scatter_kernel<__nv_bfloat16, 4, false>, (__nv_bfloat16*)dX) : go(head_scatter_kernel<__nv_bfloat16, 1, false>, (__nv_bfloat16*)dX);
 }

@@ -15,6 +15,8 @@ struct HeadRows {
   float *k, *sum;             // softmax statistics
   float* total;               // [2] loss, counted tokens
   void* x;                    // the products' rows of X, zeros behind them to whole tiles
+  int64_t x_rows;             // how many it has
+  int second;                 // where the same rows lie again (0: nowhere)
 };
 
 // Products at the targets formed again in 64 bits by the kernel that brings the rows together (bf16, few of them): z [entry][row] null: not.

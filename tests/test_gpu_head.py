@@ -317,6 +317,26 @@ def test_confident_and_large_logits(dtype, tied):
     compare(c, inp, run, ref)
 
 
+@pytest.mark.parametrize("top_k", [0, 5])
+@pytest.mark.parametrize("tied", [False, True], ids=["dv", "vd"])
+@pytest.mark.parametrize("tile", [None, "0", "1", "2", "3", "4"])
+def test_few_tokens_gradients_are_off_by_their_own_rounding(monkeypatch, tile, tied, top_k):
+    """Up to 64 padded rows dz comes in two parts, so that what is left in the norm is the results' rounding, at most half a step each and
+    2^-8 / sqrt(3) in the rms, and what the error of p leaves (dz in one part: another rounding of every value, 2.3e-3 to 3.5e-3 in all)."""
+    if tile:
+        monkeypatch.setenv("FBL_HEAD_TILE", tile)
+    for batch, seq, d, vocab in ((1, 1, 256, 700), (1, 64, 128, 515), (3, 13, 192, 2050), (8, 1, 320, 64)):
+        c = cfg(batch, seq, d, vocab, "bf16", tied, top_k)
+        run, inp = run_and_compare(c, ignored=0.2 if seq > 1 else 0.0, weighted=seq == 13)
+        ref = orc.head_fwd_bwd(c, inp)
+        s, n = dz_slack(c, inp, ref), batch * seq
+        x, w = np.abs(inp["X"].reshape(n, -1)), np.abs(inp["W"].T if tied else inp["W"])
+        for name, slack in (("dX", s @ w.T), ("dW", (s.T @ x) if tied else x.T @ s)):
+            want = ref[name].reshape(-1)
+            off = np.linalg.norm(run.fetch(name).reshape(-1) - want)
+            assert off <= RMS * np.linalg.norm(want) + np.linalg.norm(slack), (name, batch, seq, off / np.linalg.norm(want))
+
+
 @pytest.mark.parametrize("top_k", [0, 3])
 @pytest.mark.parametrize("tied", [False, True], ids=["dv", "vd"])
 def test_few_tokens_targets_in_64_bits(tied, top_k):
