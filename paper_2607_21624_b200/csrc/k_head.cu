@@ -506,7 +506,8 @@ cudaError_t launch_teacher_entries(const int32_t* ids, const float* logits, int 
 cudaError_t launch_head_combine(const float2* part, int tiles, const float* z_at, const HeadRows& R, float scale, float* loss, float* total,
                                 float* block_sums, int seq, int t_pad, const HeadExact& exact, int32_t* status, cudaStream_t st) {
   const bool few = R.rows <= COMBINE_FEW;
-  return launch_pdl(head_combine_kernel, dim3(few ? 1u : (unsigned)(R.rows / 8)), dim3(few ? (unsigned)R.rows / 8 * 128 : 256), 0, st, part, tiles, z_at,
+  const unsigned threads = !few ? 256 : (unsigned)(R.rows <= 32 ? R.rows * 32 : R.rows / 8 * 128);       // a warp has a row, or two
+  return launch_pdl(head_combine_kernel, dim3(few ? 1u : (unsigned)(R.rows / 8)), dim3(threads), 0, st, part, tiles, z_at,
                     R, scale, loss, total, (float2*)block_sums, seq, t_pad, exact, status);
 }
 cudaError_t launch_head_scatter(int dtype, int sm_count, const float* acc, int areas, const HeadRows& R, int d_model, const float* over, float alpha,
