@@ -84,8 +84,8 @@ template <bool TARGETS>
 __global__ void __launch_bounds__(256) head_rows_kernel(const int32_t* __restrict__ targets, HeadRows R, int seq, int t_pad, int vocab, int per,
                                                         const uint4* __restrict__ X, uint4* __restrict__ Xc, int all_panels, const HeadExact exact, int32_t* status) {
   __shared__ int s_before[8], s_pos[32], s_count;
-  pdl_launch_dependents();
   pdl_wait();
+  pdl_launch_dependents();      // after the wait: the product behind may ask for weights early, and what wrote them is complete then
   const int groups = (all_panels + ROWS_PANELS - 1) / ROWS_PANELS;
   if ((int)blockIdx.y >= groups) {             // the blocks behind those that copy
     exact_products<TARGETS>(exact, targets, R, seq, t_pad, vocab, X, (blockIdx.y - groups) * gridDim.x + blockIdx.x, (gridDim.y - groups) * gridDim.x);
