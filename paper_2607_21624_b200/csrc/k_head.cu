@@ -293,6 +293,7 @@ __device__ __forceinline__ float scaled(float k, float s, float top, float c) { 
 // asked for at once (of rows without a loss, too, whose partials are nothing), and up to 64 rows are one block's, which adds its
 // losses up itself; of several blocks the one that ends last does, two latencies later.
 constexpr int COMBINE_FEW = 64;
+template <bool EXACT>
 __global__ void __launch_bounds__(1024) head_combine_kernel(const float2* __restrict__ part, int tiles, const float* __restrict__ z_at,
                                                             HeadRows R, float scale, float* __restrict__ loss, float* __restrict__ total,
                                                             float2* __restrict__ block_sums, int seq, int t_pad, const HeadExact exact, int32_t* status) {
@@ -315,7 +316,7 @@ __global__ void __launch_bounds__(1024) head_combine_kernel(const float2* __rest
     };
     load(0);
     const float y0 = R.y[row], z0 = __ldcg(z_at + row), constant = R.constant[row];      // entry 0, which lane 0 takes
-    const double x0 = exact.z ? __ldcg(exact.z + row) : 0.0;
+    const double x0 = EXACT ? __ldcg(exact.z + row) : 0.0;
     const int count = R.count[row];
     float l = 0.f;
     if (count != 0) {
@@ -344,7 +345,7 @@ __global__ void __launch_bounds__(1024) head_combine_kernel(const float2* __rest
       for (int e = lane; e < count; e += 32) {
         const float y = e ? R.y[(int64_t)e * R.rows + row] : y0, z = e ? __ldcg(z_at + (int64_t)e * R.rows + row) : z0;
         if (y != 0.f) toward = fmaf(y, (k - z) * scale, toward);
-        if (exact.z) {
+        if (EXACT) {
           const double x = e ? __ldcg(exact.z + (int64_t)e * R.rows + row) : x0;
           const float off = (float)(x * exact.unlift - (double)z) * scale;
           if (fabsf(off) < 1.f) {           // (of infinities, none)
@@ -356,7 +357,7 @@ __global__ void __launch_bounds__(1024) head_combine_kernel(const float2* __rest
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) toward += __shfl_xor_sync(0xffffffffu, toward, o);
       l = fmaf(LN2, toward, logf(s)) + constant;
-      if (exact.z) {
+      if (EXACT) {
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) more += __shfl_xor_sync(0xffffffffu, more, o);
         l += log1pf(more / s);
@@ -507,8 +508,8 @@ cudaError_t launch_head_combine(const float2* part, int tiles, const float* z_at
                                 float* block_sums, int seq, int t_pad, const HeadExact& exact, int32_t* status, cudaStream_t st) {
   const bool few = R.rows <= COMBINE_FEW;
   const unsigned threads = !few ? 256 : (unsigned)(R.rows <= 32 ? R.rows * 32 : R.rows / 8 * 128);       // a warp has a row, or two
-  return launch_pdl(head_combine_kernel, dim3(few ? 1u : (unsigned)(R.rows / 8)), dim3(threads), 0, st, part, tiles, z_at,
-                    R, scale, loss, total, (float2*)block_sums, seq, t_pad, exact, status);
+  return launch_pdl(exact.z ? head_combine_kernel<true> : head_combine_kernel<false>, dim3(few ? 1u : (unsigned)(R.rows / 8)), dim3(threads), 0, st,
+                    part, tiles, z_at, R, scale, loss, total, (float2*)block_sums, seq, t_pad, exact, status);
 }
 cudaError_t launch_head_scatter(int dtype, int sm_count, const float* acc, int areas, const HeadRows& R, int d_model, const float* over, float alpha,
                                 void* dX, cudaStream_t st) {
