@@ -127,7 +127,8 @@ __device__ __forceinline__ void stats64(const HeadEpi& H, Row<false>& R, uint32_
     for (int i = 0; i < 4; ++i) top[i] = tc::fmax3(top[i], __uint_as_float(v[j + i]), __uint_as_float(v[j + 4 + i]));
   const float was = k;
   k = fmaxf(k, tc::fmax3(top[0], top[1], fmaxf(top[2], top[3])));
-  const float2 mk = make_float2(-k, -k), c2 = make_float2(H.scale, H.scale);
+  const float from = k == -INFINITY ? 0.f : k;            // so far nothing but -inf, whose distances from one another are NaN and not a sum of 0
+  const float2 mk = make_float2(-from, -from), c2 = make_float2(H.scale, H.scale);
   float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
   for (int j = 0; j < 64; j += 2) {
@@ -135,7 +136,7 @@ __device__ __forceinline__ void stats64(const HeadEpi& H, Row<false>& R, uint32_
     sum[j / 2 % 2] = __fadd2_rn(sum[j / 2 % 2], make_float2(tc::fast_exp2(x.x), tc::fast_exp2(x.y)));
   }
   sum[0] = __fadd2_rn(sum[0], sum[1]);
-  s = s * tc::fast_exp2((was - k) * H.scale) + (sum[0].x + sum[0].y);
+  s = s * tc::fast_exp2((was - from) * H.scale) + (sum[0].x + sum[0].y);
 }
 
 // 64 columns of logits become their gradient.

@@ -317,6 +317,43 @@ def test_confident_and_large_logits(dtype, tied):
     compare(c, inp, run, ref)
 
 
+@pytest.mark.parametrize("kind", ["infinite", "overflow"])
+@pytest.mark.parametrize("top_k", [0, 4])
+@pytest.mark.parametrize("dtype,tile", [("bf16", t) for t in (None, "0", "1", "2", "3", "4")] + [("fp32", t) for t in ("64", "128")],
+                         ids=lambda v: str(v))
+def test_logits_of_minus_infinity(monkeypatch, dtype, tile, top_k, kind):
+    """Columns whose logits are -inf, from weights of -inf or from products past the range of fp32, panels of 64 and tiles of 256 of them
+    and single ones, are columns that are not there: everything else is what a vocabulary without them gives."""
+    if tile:
+        monkeypatch.setenv("FBL_HEAD_TILE" if dtype == "bf16" else "FBL_F32_BN", tile)
+    v = 1100
+    gone = np.zeros(v, dtype=bool)
+    gone[:130] = gone[256:512] = gone[640:704] = True                    # the first panels of a row, too
+    gone[[200, 530, 999, 1099]] = True
+    kept = np.flatnonzero(~gone)
+    for batch, seq in ((1, 20), (2, 150)):
+        few = cfg(batch, seq, 128, len(kept), dtype, top_k=top_k)
+        inp = make_head_inputs(few, ignored=0.2)
+        inp["X"][..., 0], inp["W"][0] = (1.0 if kind == "infinite" else 2.0 ** 64), 0.0
+        ref = orc.head_fwd_bwd(few, inp)
+        c = cfg(batch, seq, 128, v, dtype, top_k=top_k)
+        W = np.zeros((128, v))
+        W[:, kept], W[0, gone] = inp["W"], -np.inf if kind == "infinite" else -2.0 ** 70
+        names = "top_ids" if top_k else "targets"
+        run = HeadRunner(c, guard_bytes=4096)
+        run.load_inputs({**inp, "W": W, names: np.where(inp[names] < 0, -1, kept[np.maximum(inp[names], 0)]).astype(np.int32)})
+        run.step()
+        loss = run.fetch("loss").reshape(batch, seq)
+        assert (np.abs(loss - ref["loss"]) <= loss_bound(few, inp, ref)).all() and (loss[~ref["has"]] == 0).all()
+        # dX along the first column is 0 times -inf where there are such weights; dW along it has hidden states of 2^64
+        n, dz, slack = batch * seq, ref["dZ"], dz_slack(few, inp, ref)
+        x, w = inp["X"].reshape(n, -1).T[1:], inp["W"].T[:, 1:]
+        dX, dW = run.fetch("dX").reshape(n, -1), run.fetch("dW")
+        check_grad("dX", c, dX[:, 1:], ref["dX"].reshape(n, -1)[:, 1:], dz, w, c.vocab, slack @ np.abs(w))
+        check_grad("dW", c, dW[1:, kept], ref["dW"][1:], x, dz, n, np.abs(x) @ slack)
+        assert (dW[:, gone] == 0).all() and run.status() == 0 and run.guards_intact() == []
+
+
 @pytest.mark.parametrize("top_k", [0, 5])
 @pytest.mark.parametrize("tied", [False, True], ids=["dv", "vd"])
 @pytest.mark.parametrize("tile", [None, "0", "1", "2", "3", "4"])
