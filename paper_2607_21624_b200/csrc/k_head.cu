@@ -209,7 +209,7 @@ __global__ void __launch_bounds__(32 * ENTRY_WARPS) teacher_entries_kernel(const
     const int id = in ? ids[at + e] : -1;
     const float z = in ? logits[at + e] : 0.f;
     key[j] = id >= 0 ? (uint32_t)id * 128u + (uint32_t)e : NO_KEY;
-    p[j] = id >= 0 ? z / temperature : -INFINITY;
+    p[j] = id >= 0 ? z : -INFINITY;
     bad = bad || id >= vocab || p[j] != p[j];
     top = fmaxf(top, p[j]);
   }
@@ -221,7 +221,7 @@ __global__ void __launch_bounds__(32 * ENTRY_WARPS) teacher_entries_kernel(const
   if (!bad && top > -INFINITY) {
     float sum = 0.f;
 #pragma unroll
-    for (int j = 0; j < PER; ++j) { p[j] = expf(p[j] - top); sum += p[j]; }
+    for (int j = 0; j < PER; ++j) { p[j] = expf((p[j] - top) / temperature); sum += p[j]; }      // (a quotient alone may leave fp32, and is rounded at its own size)
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
 #pragma unroll

@@ -274,6 +274,41 @@ def test_teachers_lists(dtype):
     assert run.guards_intact() == [] and run.status() == 0
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("tau", [0.5, 1e-30, 3.0, 1e30])
+def test_teachers_large_logits_and_temperatures(tau, dtype):
+    """Finite logits have a loss at any temperature, also where a logit / temperature leaves fp32, and count by their distances, also where
+    those are a step of fp32 beside the logits themselves.  Weights of zero: a loss is log vocab - entropy of the list, whose probabilities
+    are off by 2^-24 of a distance of at most 160 (beyond, a probability is below 2^-126 and zero in fp32), and by expf's two steps."""
+    c = cfg(1, 24, 64, 200, dtype, top_k=6, tau=tau)
+    inp = make_head_inputs(c)
+    inp["W"][:] = 0.0
+    ids, lg = inp["top_ids"][0], inp["top_logits"][0]
+    ids[:] = [3, 17, 64, 128, 199, 0]
+    lg[0] = [3e38, -3e38, 3e38, 0, 0, 0]
+    lg[1] = -3e38                                   # finite, equal: a loss
+    lg[2] = [-3e38, -3e38, -np.inf, -np.inf, -np.inf, -np.inf]
+    lg[3] = [3e38, 3e38, 3e38, 3e38, 3e38, 3e38]
+    for i in range(4, 24):                          # 1e4 to 1e5, a few apart
+        lg[i] = np.float32(1e4 * 1.13 ** (i - 4) * (-1 if i % 3 == 0 else 1)) + np.float32([0, 1, -1, 2, 0.5, -0.25])
+    ids[23, 2], lg[23, 2] = -1, 3e38                # not there
+    lg[:] = lg.astype(np.float32)
+    ref = orc.head_fwd_bwd(c, inp)
+    y, has = orc.targets(c, inp)
+    assert has.all()
+    run = HeadRunner(c, guard_bytes=4096)
+    run.load_inputs(inp)
+    run.step()
+    with np.errstate(divide="ignore", invalid="ignore"):
+        terms = np.where(y > 0, y * (1 + np.abs(np.log(y))), 0.0).sum(1)
+    off = np.abs(run.fetch("loss") - ref["loss"][0])
+    assert (off <= terms * 160 * 2.0 ** -24 + 8 * 2.0 ** -24 * np.log(200) + 2.0 ** -20).all(), off.max()
+    assert run.fetch("total")[1] == 24 and run.guards_intact() == [] and run.status() == 0
+    assert (run.fetch("dX") == 0).all()
+    x, dz = inp["X"].reshape(24, -1).T, ref["dZ"]
+    check_grad("dW", c, run.fetch("dW") * min(tau, 1.0), ref["dW"] * min(tau, 1.0), x, dz * min(tau, 1.0), 24, np.abs(x) @ (np.abs(dz) + y / 24 / tau) * min(tau, 1.0) * 2.0 ** -16)
+
+
 def test_one_teacher_logit_is_a_label_bit_for_bit():
     a, b = cfg(2, 100, 128, 900, top_k=1), cfg(2, 100, 128, 900)
     inp = make_head_inputs(a, ignored=0.2)
