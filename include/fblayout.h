@@ -453,7 +453,8 @@ int64_t fbl_norm_launch_count(const fbl_norm_plan* plan);
  * A label or id of vocab or more, and a teacher's logit that is NaN or +inf, make the token's loss and row of dX NaN (and dW).
  *
  * loss [batch * seq] fp32; total[0] = sum of the losses, total[1] = number of tokens with a loss (device memory, both written).
- * dloss [batch * seq] fp32, the gradient of each token's loss, or NULL: 1 / total[1], the gradient of the mean.  dX or dW may be
+ * dloss [batch * seq] fp32, the gradient of each token's loss (of tokens without one it is not looked at), or NULL: 1 / total[1], the
+ * gradient of the mean.  A factor that the weights have in common is not rounded with dz.  dX or dW may be
  * NULL: then that gradient is not formed (a frozen head; a frozen model).  The backward takes the X and W that the forward
  * had, and from `saved` the targets' entries, the softmax statistics and the rows of X with a loss, which the forward has brought
  * together there; `saved` serves any number of backward calls.  Outputs overlap no input and no workspace (dW is written while W

@@ -114,6 +114,7 @@ struct HeadEpi {
   float* z_at;                  // forward: [entry][row] the products at the targets
   const float *k, *sum;         // backward: the row's k and sum
   const float *dloss, *over;    // backward: the gradient of each token's loss [batch * seq], or else 1 / max(*over, 1), or else 1
+  const float* raise;           // dloss times *raise, where not null
   float inv_tau;
   int second;                   // backward: products' rows from here on are the first ones again, and get what dz loses by its rounding (0: none)
 };

@@ -78,7 +78,7 @@ struct fbl_head_plan {
   size_t sv_ids, sv_y, sv_count, sv_constant, sv_row_of, sv_pos, sv_n, sv_k, sv_sum, sv_total, sv_x, saved_bytes;
   bool exact;                   // products at the targets formed again in 64 bits
   size_t sf_part, sf_z, sf_blocks, sf_exact, scratch_fwd_bytes;
-  size_t sb_dz, sb_acc, scratch_bwd_bytes;
+  size_t sb_raise, sb_dz, sb_acc, scratch_bwd_bytes;
   mutable int64_t launches;
 };
 struct fbl_norm_plan {
@@ -274,6 +274,7 @@ int fbl_head_plan_create(const fbl_head_desc* desc, fbl_head_plan** out) {
   p->sf_exact = take(o, p->exact ? n * p->top_k * 8 : 0);
   p->scratch_fwd_bytes = o;
   o = FBL_ALIGN;
+  p->sb_raise = take(o, 4);
   p->sb_dz = take(o, piece_bytes);
   p->sb_acc = take(o, (size_t)p->x_rows * d.d_model * 4 * p->slices);
   p->scratch_bwd_bytes = o;
@@ -377,7 +378,13 @@ int fbl_head_bwd(const fbl_head_plan* p, const void* X, const void* W, const flo
   float* acc = (float*)(sc + p->sb_acc);
   const bool bf16 = p->d.dtype == FBL_DTYPE_BF16;
   const int D = p->d.d_model;
-  const float inv_tau = 1.f / p->d.temperature, *over = dloss ? nullptr : R.total + 1;
+  const float inv_tau = 1.f / p->d.temperature;
+  // what the products of a bf16 dz are divided by: the mean's number of tokens and temperature, or what weights were multiplied by (of few
+  // rows, whose dz comes in two parts, they are not)
+  float* raise = bf16 && dloss && !p->second ? (float*)(sc + p->sb_raise) : nullptr;
+  const float* over = dloss ? raise : R.total + 1;
+  const float alpha = dloss ? 1.f : inv_tau;
+  if (raise) HEAD_STEP(launch_head_weights(dloss, R, p->d.seq, p->base->t_pad, inv_tau, raise, st));
   for (int col0 = 0; col0 < p->cols; col0 += p->piece) {
     const int cols = p->cols - col0 < p->piece ? p->cols - col0 : p->piece;
     {
@@ -386,7 +393,7 @@ int fbl_head_bwd(const fbl_head_plan* p, const void* X, const void* W, const flo
       g.reset_status = col0 == 0;
       g.epi = 7;
       g.head = epilogue_of(p, R, col0);
-      g.head.dloss = dloss;
+      g.head.dloss = dloss; g.head.raise = raise;
       g.head.tile = p->grad_tile;
       if (!bf16) g.head.over = over;
       HEAD_RUN(run_products(p, &g, 1, status, st));
@@ -401,7 +408,7 @@ int fbl_head_bwd(const fbl_head_plan* p, const void* X, const void* W, const flo
       g.t[0].b = p->d.vocab_rows ? R.x : dz;
       g.c_rows = piece_rows(p, col0, cols);
       g.c = (void*)weights_at(p, dW, col0);
-      if (bf16) { g.over = over; g.alpha = inv_tau; }          // the mean's gradient, see head_epilogue.cuh
+      if (bf16) { g.over = over; g.alpha = alpha; }
     }
     if (dX) {
       GemmArgs& g = gs[count++];
@@ -415,7 +422,7 @@ int fbl_head_bwd(const fbl_head_plan* p, const void* X, const void* W, const flo
     }
     HEAD_RUN(run_products(p, gs, count, status, st));
   }
-  if (dX) HEAD_STEP(launch_head_scatter(p->d.dtype, p->base->sm_count, acc, p->slices, R, D, bf16 ? over : nullptr, inv_tau, dX, st));
+  if (dX) HEAD_STEP(launch_head_scatter(p->d.dtype, p->base->sm_count, acc, p->slices, R, D, bf16 ? over : nullptr, alpha, dX, st));
   return FBL_OK;
 }
 

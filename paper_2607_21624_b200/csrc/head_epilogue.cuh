@@ -5,7 +5,8 @@
 //   forward   k = max z,  s = sum of 2^(c (z - k))  over a tile's columns, and z itself at the row's targets
 //   backward  dz = (g / s) 2^(c (z - k)) - g y,  g = the loss's gradient / temperature, y the target probability of the column
 //             (bf16: g = 1 for the mean loss, whose 1 / (tokens x temperature) the two products behind are scaled by: with it in dz every
-//             token's target would be rounded the same way, and dX and dW come out too large or too small by up to 2^-9)
+//             token's target would be rounded the same way, and dX and dW come out too large or too small by up to 2^-9; weights that the
+//             caller gives are multiplied by a common factor of 1 to 2 for the same reason, head_weights_kernel)
 // k and s are a whole row's by then (head_combine_kernel).  Logits only ever enter as distances from the row's largest: a target that
 // holds all of its row's probability gives log s = log 1 exactly, and logits of any size have a loss.  Sums are fp32; dz is
 // rounded to the storage type, as an operand of the two products that consume it (bf16: half a step of 2^-8 of each value, as
@@ -89,8 +90,10 @@ struct Row {
     float scale = H.inv_tau, sum = 1.f;
     if (GRAD) {
       const int b = row / t_pad, t = row - b * t_pad;
-      if (H.dloss) scale *= t < seq ? H.dloss[(long long)b * seq + t] : 0.f;
-      else scale = H.over ? scale / fmaxf(*H.over, 1.f) : 1.f;
+      if (H.dloss) {
+        scale *= t < seq ? H.dloss[(long long)b * seq + t] : 0.f;
+        if (H.raise) scale *= __ldcg(H.raise);
+      } else scale = H.over ? scale / fmaxf(*H.over, 1.f) : 1.f;
       k = H.k[row];
       sum = H.sum[row];
     }

@@ -415,6 +415,37 @@ __global__ void __launch_bounds__(1024) head_combine_kernel(const float2* __rest
   }
 }
 
+// Losses of equal weight -- 1 / tokens given as weights, a loss scale, weights of 0 and 1 / tokens -- put one factor into dz, and where a
+// target's probability is small its entry is that factor, which bf16 rounds the same way in every token: dX and dW come out too large or too small by
+// up to 2^-9 (1/788: by 0.2 %).  So the largest weight of a token with a loss is made a power of two, by a factor of 1 to 2 that the products'
+// epilogues take out again in fp32, and equal weights round as a mean's 1 does.  One block, since a maximum of a few thousand weights is a
+// handful of memory latencies (a launch of its own all the same: 2048 tokens of 768 over 50257 columns 458 -> 462 us a step).
+__global__ void __launch_bounds__(1024) head_weights_kernel(const float* __restrict__ dloss, HeadRows R, int seq, int t_pad, float inv_tau, float* __restrict__ raise) {
+  __shared__ float s_top[32];
+  pdl_wait();
+  pdl_launch_dependents();      // after the wait: the product behind may ask for weights early, and what wrote them is complete then
+  float top = 0.f;
+#pragma unroll 8
+  for (int row = threadIdx.x; row < (int)R.rows; row += 1024) {
+    const int b = row / t_pad, t = row - b * t_pad;
+    const float w = t < seq ? fabsf(dloss[(int64_t)b * seq + t]) : 0.f;
+    if (R.count[row] != 0 && w < INFINITY) top = fmaxf(top, w);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  if (threadIdx.x % 32 == 0) s_top[threadIdx.x / 32] = top;
+  __syncthreads();
+  if (threadIdx.x >= 32) return;
+  top = s_top[threadIdx.x];
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  if (threadIdx.x) return;
+  top *= inv_tau;
+  int e;
+  const float m = frexpf(top, &e);                             // in [1/2, 1)
+  *raise = top > 0.f && top < 0x1p127f ? 1.f / m : 1.f;
+}
+
 // dX: the areas' sums (of a row and its second, where there are such) times alpha / max(*over, 1) where `over` is not null, at the tokens' own rows, and zeros at the rows without a
 // loss.  A warp has 128 consecutive bytes of sums: with GROUPS = 4 its quarters take every fourth area each and are added up in
 // that order (few elements and many areas: 56 x 768 of 24 areas), with 1 four pieces of 128 bytes.  Bound by memory.
@@ -510,6 +541,9 @@ cudaError_t launch_head_combine(const float2* part, int tiles, const float* z_at
   const unsigned threads = !few ? 256 : (unsigned)(R.rows <= 32 ? R.rows * 32 : R.rows / 8 * 128);       // a warp has a row, or two
   return launch_pdl(exact.z ? head_combine_kernel<true> : head_combine_kernel<false>, dim3(few ? 1u : (unsigned)(R.rows / 8)), dim3(threads), 0, st,
                     part, tiles, z_at, R, scale, loss, total, (float2*)block_sums, seq, t_pad, exact, status);
+}
+cudaError_t launch_head_weights(const float* dloss, const HeadRows& R, int seq, int t_pad, float inv_tau, float* raise, cudaStream_t st) {
+  return launch_pdl(head_weights_kernel, dim3(1), dim3(1024), 0, st, dloss, R, seq, t_pad, inv_tau, raise);
 }
 cudaError_t launch_head_scatter(int dtype, int sm_count, const float* acc, int areas, const HeadRows& R, int d_model, const float* over, float alpha,
                                 void* dX, cudaStream_t st) {

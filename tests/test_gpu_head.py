@@ -472,6 +472,80 @@ def test_fp32_operands_beyond_the_parts_range(monkeypatch, tied):
     assert fp32_err(dX[same], plain.fetch("dX")[same]) <= 1e-5
 
 
+@pytest.mark.parametrize("tied", [False, True], ids=["dv", "vd"])
+@pytest.mark.parametrize("batch,seq,share", [(4, 197, 1.0), (1, 333, 1.0), (6, 61, 0.5), (3, 20, 1.0)], ids=str)
+@pytest.mark.parametrize("top_k,tau", [(0, 1.0), (1, 3.0)], ids=["labels", "teacher"])
+def test_equal_weights_leave_no_common_factor(batch, seq, share, top_k, tau, tied):
+    """1 / n given as every token's weight, or every other one's and 0 for the rest: dX and dW are those of the mean, no factor larger or
+    smaller.  A target's entry of dz is 1 - p of its weight, which comes out as the weight where p is below 2^-9: off by p.  Beside it stand 6000
+    entries of some p, rounded independently (RMS p sqrt(6000) < 1e-4 of it) and the results' roundings, RMS / sqrt(n d) < 5e-5.
+    (1/788, 1/333, 1/366 and 1/1098 in bf16 are 2.0e-3 to 6e-4 off.)"""
+    c = cfg(batch, seq, 64, 6000, "bf16", tied, top_k, tau, w_std=0.02)
+    inp = make_head_inputs(c)
+    n = batch * seq
+    if top_k:
+        inp["top_ids"] = np.maximum(inp["top_ids"], 0)
+    else:
+        inp["targets"] = np.maximum(inp["targets"], 0)
+    on = (np.arange(n) % 2 == 0).reshape(batch, seq) if share < 1 else np.ones((batch, seq), dtype=bool)
+    inp["dloss"] = np.where(on, 1.0 / n, 0.0).astype(np.float32).astype(np.float64)
+    ref = orc.head_fwd_bwd(c, inp)
+    run = HeadRunner(c, guard_bytes=4096)
+    run.load_inputs(inp)
+    run.step()
+    got = {k: run.fetch(k) for k in ("dX", "dW")}
+    y, _ = orc.targets(c, inp)
+    p = np.exp(ref["Z"] - ref["lse"][:, None])[y > 0]
+    for k, v in got.items():
+        factor = (v * ref[k]).sum() / (ref[k] ** 2).sum()
+        assert abs(factor - 1) <= p.max() + 1.5e-4, (k, factor - 1)
+    if share == 1:
+        # against the mean's path: weights a step of fp32 apart change a rounding, one bf16 step of at most 2^-7, in less than one of 2^13
+        # elements of dz and of the results (few rows, in two parts: the results')
+        run.load_inputs({**inp, "dloss": None})
+        run.step()
+        for k, v in got.items():
+            mean = run.fetch(k)
+            assert np.linalg.norm(v - mean) <= 2.5e-4 * np.linalg.norm(mean), (k, np.linalg.norm(v - mean) / np.linalg.norm(mean))
+    assert run.status() == 0 and run.guards_intact() == []
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("size", [1e-30, 1e36, 0.0])
+def test_weights_of_any_size(size, dtype):
+    """Weights at the ends of fp32's range, and what tokens without a loss have for one, which is not looked at; a weight of NaN is its
+    token's alone."""
+    c = cfg(3, 45, 128, 700, dtype, w_std=0.02)
+    inp = make_head_inputs(c, ignored=0.4, weighted=True)
+    inp["dloss"] = (inp["dloss"] * size).astype(np.float32).astype(np.float64)
+    ref = orc.head_fwd_bwd(c, inp)
+    run = HeadRunner(c, guard_bytes=4096)
+    run.load_inputs(inp)
+    run.step()
+    assert np.isfinite(run.fetch("dX")).all() and np.isfinite(run.fetch("dW")).all()
+    if size:
+        scaled = {**ref, "dX": ref["dX"] / size, "dW": ref["dW"] / size}
+        for k in ("dX", "dW"):
+            off = np.linalg.norm(run.fetch(k) / size - scaled[k]) / np.linalg.norm(scaled[k])
+            assert off <= (2 * RMS if dtype == "bf16" else 1e-5), (k, off)
+    else:
+        assert (run.fetch("dX") == 0).all() and (run.fetch("dW") == 0).all()
+    want = {k: run.fetch(k) for k in ("loss", "dX", "dW")}
+    has = ref["has"].reshape(-1)
+    for junk in (np.inf, np.nan, -3e38):
+        run.load_inputs({**inp, "dloss": np.where(ref["has"], inp["dloss"], junk)})
+        run.step()
+        for k, v in want.items():
+            assert np.array_equal(v, run.fetch(k)), (k, junk)
+    bad = inp["dloss"].copy()
+    bad.reshape(-1)[np.flatnonzero(has)[5]] = np.nan
+    run.load_inputs({**inp, "dloss": bad})
+    run.step()
+    dX, same = run.fetch("dX").reshape(135, -1), np.arange(135) != np.flatnonzero(has)[5]
+    assert np.isnan(dX[~same]).all() and np.isfinite(dX[same]).all() and np.isnan(run.fetch("dW")).all()
+    assert run.guards_intact() == [] and run.status() == 0
+
+
 def test_bits_repeat_on_dirty_work_areas():
     for c in (cfg(2, 300, 256, 5003, tied=True), cfg(4, 77, 128, 1500, top_k=32, tau=2.0), cfg(2, 150, 128, 1500, "fp32")):
         inp = make_head_inputs(c, ignored=0.3)
