@@ -412,7 +412,8 @@ int fbl_xattn_bwd(const fbl_plan* plan, const void* dY, const void* X, const voi
  *   forward   Y = gamma (X - mean) rstd + beta (LayerNorm), Y = gamma X rstd with rstd of the mean square (RMSNorm)
  *   backward  dX; dgamma = sum over the tokens of dY xhat, dbeta = sum of dY (fp32, two stages, no atomics: the same bits
  *             every time).  dgamma and dbeta may both be NULL (the norm's parameters are frozen); dbeta is NULL for RMSNorm.
- * `saved` carries (mean, rstd) of every padded token row; scratch_bwd holds the partial rows of the token-axis sums.
+ * `saved` carries (mean, rstd) of every padded token row; scratch_bwd holds the partial rows of the token-axis sums.  No wait of these
+ * calls can expire, so there is no status word: the forward takes a scratch as the others do and leaves it as it is.
  * Pointers, alignment, padding, streams and return codes as for the attention layer's calls.  gamma and beta are read before
  * the launch in front has completed, as inputs of the step: no kernel of this library writes them. */
 typedef struct {

@@ -252,8 +252,7 @@ cudaError_t launch_rope(const fbl_plan* p, void* A, int heads_a, void* B, int he
 cudaError_t launch_norm_fwd(const fbl_plan* p, const void* X, const float* gamma, const float* beta, void* Xn,
                             float* stats, int32_t* status, cudaStream_t st, float2* rope = nullptr);
 // The forward of the norm as an operator of its own: the same, or a kernel for many wide rows.
-cudaError_t launch_norm_op_fwd(const fbl_plan* p, const void* X, const float* gamma, const float* beta, void* Y, float* stats, int32_t* status,
-                               cudaStream_t st);
+cudaError_t launch_norm_op_fwd(const fbl_plan* p, const void* X, const float* gamma, const float* beta, void* Y, float* stats, cudaStream_t st);
 // Token-axis column sums of up to four matrices: slabs of 256 rows are summed to one row of partials each (at part[i],
 // slabs x cols), which a second kernel adds up.
 struct ColsumGroup {

@@ -480,7 +480,7 @@ int fbl_norm_fwd(const fbl_norm_plan* p, const void* X, const float* gamma, cons
   if (p->d.norm == FBL_NORM_LAYERNORM && !beta) return FBL_ERR_INVALID_ARG;
   const void* ptrs[] = {X, Y, saved, scratch};
   for (const void* q : ptrs) if (misaligned(q)) return FBL_ERR_MISALIGNED;
-  HEAD_STEP(launch_norm_op_fwd(p->base, X, gamma, beta, Y, (float*)saved, (int32_t*)scratch, as_stream(stream)));
+  HEAD_STEP(launch_norm_op_fwd(p->base, X, gamma, beta, Y, (float*)saved, as_stream(stream)));
   return FBL_OK;
 }
 

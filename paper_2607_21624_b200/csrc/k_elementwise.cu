@@ -236,8 +236,8 @@ __global__ void __launch_bounds__(512) norm_fwd_kernel(const T* __restrict__ X, 
   constexpr int V = Vec16<T>::N, TW = tile_w_of<T>::value;
   __shared__ __align__(16) float s_ex[2 * NORM_EX];
   // First kernel of the forward pass: it resets the pass's status word (later kernels only write it after a
-  // bounded wait of about a second has expired), which saves a fill node in front of the pass.
-  if (blockIdx.x == 0 && threadIdx.x == 0) *status = 0;
+  // bounded wait of about a second has expired), which saves a fill node in front of the pass.  The norm as an operator has none.
+  if (status && blockIdx.x == 0 && threadIdx.x == 0) *status = 0;
   pdl_launch_dependents();
   if ((int)blockIdx.x >= n_norm) {                           // blocks behind the norm's: the rotary embedding's table
     pdl_wait();
@@ -332,11 +332,10 @@ __host__ __device__ constexpr int rows_stages(int nv) { return nv > 8 ? 2 : nv >
 template <typename T, int NV>
 __global__ void __launch_bounds__(32 * ROWS_WARPS, 1) norm_rows_kernel(const T* __restrict__ X, const float* __restrict__ gamma, const float* __restrict__ beta,
                                                            T* __restrict__ Y, float* __restrict__ stats, int64_t n_pad, int d, int seq, int t_pad,
-                                                           int rms, float eps, int32_t* __restrict__ status) {
+                                                           int rms, float eps) {
   constexpr int V = Vec16<T>::N, TW = tile_w_of<T>::value;
   constexpr int S = rows_stages(NV);
   extern __shared__ __align__(16) float s_params[];           // gamma, beta; the warps' rings [stage][vector][lane]
-  if (blockIdx.x == 0 && threadIdx.x == 0) *status = 0;
   pdl_launch_dependents();
   for (int c = threadIdx.x; c < d; c += 32 * ROWS_WARPS) {    // inputs of the step, as above
     s_params[c] = gamma[c];
@@ -1007,27 +1006,26 @@ cudaError_t launch_rope_bwd_round(const fbl_plan* p, const float* acc, void* dQ,
 }
 
 template <typename T, int NV>
-cudaError_t norm_rows_launch(const fbl_plan* p, const void* X, const float* gamma, const float* beta, void* Y, float* stats, int32_t* status, cudaStream_t st) {
+cudaError_t norm_rows_launch(const fbl_plan* p, const void* X, const float* gamma, const float* beta, void* Y, float* stats, cudaStream_t st) {
   static SmemLimit limit;
   const unsigned blocks = (unsigned)min((int64_t)p->sm_count, (p->n_pad + ROWS_WARPS - 1) / ROWS_WARPS);
   const size_t smem = (size_t)p->d.d_model * sizeof(float) * (beta ? 2 : 1) + (size_t)ROWS_WARPS * rows_stages(NV) * NV * 512;
   const cudaError_t e = limit.raise(norm_rows_kernel<T, NV>, smem);
   if (e != cudaSuccess) return e;
   return launch_pdl(norm_rows_kernel<T, NV>, dim3(blocks), dim3(32 * ROWS_WARPS), smem, st, (const T*)X, gamma, beta, (T*)Y, stats,
-                    p->n_pad, p->d.d_model, p->d.seq, p->t_pad, (int)(p->d.norm == FBL_NORM_RMSNORM), p->d.eps, status);
+                    p->n_pad, p->d.d_model, p->d.seq, p->t_pad, (int)(p->d.norm == FBL_NORM_RMSNORM), p->d.eps);
 }
-cudaError_t launch_norm_op_fwd(const fbl_plan* p, const void* X, const float* gamma, const float* beta, void* Y, float* stats, int32_t* status,
-                               cudaStream_t st) {
+cudaError_t launch_norm_op_fwd(const fbl_plan* p, const void* X, const float* gamma, const float* beta, void* Y, float* stats, cudaStream_t st) {
   if (p->d.norm == FBL_NORM_RMSNORM) beta = nullptr;
   const int nvec = p->d.d_model / (p->d.dtype == FBL_DTYPE_FP32 ? 4 : 8);
   // (us, a block a row and a warp a row)  fp32: 592 x 2048 4.6, 5.6; 1665 x 1280 9.8, 6.0; 8192 x 2048 35.8, 26.0.  bf16, with twice the
   // instructions a byte: 16384 x 1024 17.7, 20.0; 4096 x 2048 9.7, 10.2; 1184 x 4096 7.1, 7.7; 8192 x 4096 32.1, 28.0 (LayerNorm 35.6, 33.7)
   const bool fp32 = p->d.dtype == FBL_DTYPE_FP32;
   if (nvec > 512 || nvec <= (fp32 ? 96 : 384) || p->n_pad < (fp32 ? 8 : 24) * (int64_t)p->sm_count)
-    return launch_norm_fwd(p, X, gamma, beta, Y, stats, status, st);
-  if (!fp32) return norm_rows_launch<__nv_bfloat16, 16>(p, X, gamma, beta, Y, stats, status, st);
-  return nvec <= 128 ? norm_rows_launch<float, 4>(p, X, gamma, beta, Y, stats, status, st) : nvec <= 256 ? norm_rows_launch<float, 8>(p, X, gamma, beta, Y, stats, status, st)
-         : nvec <= 384 ? norm_rows_launch<float, 12>(p, X, gamma, beta, Y, stats, status, st) : norm_rows_launch<float, 16>(p, X, gamma, beta, Y, stats, status, st);
+    return launch_norm_fwd(p, X, gamma, beta, Y, stats, nullptr, st);
+  if (!fp32) return norm_rows_launch<__nv_bfloat16, 16>(p, X, gamma, beta, Y, stats, st);
+  return nvec <= 128 ? norm_rows_launch<float, 4>(p, X, gamma, beta, Y, stats, st) : nvec <= 256 ? norm_rows_launch<float, 8>(p, X, gamma, beta, Y, stats, st)
+         : nvec <= 384 ? norm_rows_launch<float, 12>(p, X, gamma, beta, Y, stats, st) : norm_rows_launch<float, 16>(p, X, gamma, beta, Y, stats, st);
 }
 
 cudaError_t launch_norm_fwd(const fbl_plan* p, const void* X, const float* gamma, const float* beta, void* Xn,

@@ -718,6 +718,24 @@ def test_norm(shape, dtype, norm):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("shape", [(1, 1, 64), (3, 5, 1088), (2, 1777, 3584), (1, 1665, 1280)], ids=lambda s: "x".join(map(str, s)))
+def test_norms_forward_leaves_its_scratch_alone(shape, dtype):
+    """Nobody reads a status there, and a store may land while the launch in front still uses that memory."""
+    c = cfg(*shape, 8, dtype)
+    inp = make_head_inputs(c)
+    run = NormRunner(c)
+    run.load_inputs({**inp, "dY": inp["X"]})
+    for b in (run.scratch_fwd, run.scratch):
+        b.fill_(0xC3)
+    run.forward()
+    run.torch.cuda.synchronize()
+    assert bool((run.scratch_fwd == 0xC3).all()) and bool((run.scratch == 0xC3).all())
+    run.backward()
+    run.torch.cuda.synchronize()
+    assert bool((run.scratch[:1024] == 0xC3).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("top_k,tied", [(0, True), (8, False)])
 def test_norm_and_head_together(dtype, top_k, tied):
     """The end of a step as it runs: norm, head, back through both.  What the norm's backward is given is the head's own dX, so its
