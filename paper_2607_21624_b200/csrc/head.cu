@@ -183,7 +183,7 @@ int forward(const fbl_head_plan* p, const void* W, float* loss, float* total, co
   g.head.part = part; g.head.tiles = p->tiles; g.head.z_at = z_at;
   g.head.tile = p->logits_tile;
   HEAD_RUN(run_products(p, &g, 1, status, st));
-  HEAD_STEP(launch_head_combine(part, p->tiles, z_at, R, p->scale, loss, total, (float*)(sf + p->sf_blocks), p->d.seq, p->base->t_pad,
+  HEAD_STEP(launch_head_combine(part, p->tiles, z_at, R, p->scale, loss, total, (double2*)(sf + p->sf_blocks), p->d.seq, p->base->t_pad,
                                 exact_of(p, W, sf), status, st));
   return FBL_OK;
 }
@@ -269,7 +269,7 @@ int fbl_head_plan_create(const fbl_head_desc* desc, fbl_head_plan** out) {
   o = FBL_ALIGN;                // status word
   p->sf_part = take(o, n * p->tiles * sizeof(float2));
   p->sf_z = take(o, n * p->top_k * 4);
-  p->sf_blocks = take(o, n / 8 * 8);
+  p->sf_blocks = take(o, n / 8 * sizeof(double2));
   p->exact = bf16 && p->n_pad <= EXACT_ROWS && p->n_pad * p->top_k <= EXACT_ENTRIES;
   p->sf_exact = take(o, p->exact ? n * p->top_k * 8 : 0);
   p->scratch_fwd_bytes = o;

@@ -296,7 +296,7 @@ constexpr int COMBINE_FEW = 64;
 template <bool EXACT>
 __global__ void __launch_bounds__(1024) head_combine_kernel(const float2* __restrict__ part, int tiles, const float* __restrict__ z_at,
                                                             HeadRows R, float scale, float* __restrict__ loss, float* __restrict__ total,
-                                                            float2* __restrict__ block_sums, int seq, int t_pad, const HeadExact exact, int32_t* status) {
+                                                            double2* __restrict__ block_sums, int seq, int t_pad, const HeadExact exact, int32_t* status) {
   constexpr int U = 8;
   __shared__ double s_sum[32], s_count[32];
   __shared__ int s_last;
@@ -386,7 +386,7 @@ __global__ void __launch_bounds__(1024) head_combine_kernel(const float2* __rest
     if (gridDim.x == 1) {
       publish(a, n);
     } else {
-      block_sums[blockIdx.x] = make_float2((float)a, (float)n);
+      block_sums[blockIdx.x] = make_double2(a, n);
       __threadfence();
       s_last = atomicAdd(status + HEAD_TICKET, 1) == (int)gridDim.x - 1;
     }
@@ -398,7 +398,7 @@ __global__ void __launch_bounds__(1024) head_combine_kernel(const float2* __rest
   double a = 0.0, n = 0.0;
 #pragma unroll 4
   for (int i = threadIdx.x; i < (int)gridDim.x; i += blockDim.x) {
-    const float2 v = __ldcg(block_sums + i);
+    const double2 v = __ldcg(block_sums + i);
     a += v.x;
     n += v.y;
   }
@@ -536,11 +536,11 @@ cudaError_t launch_teacher_entries(const int32_t* ids, const float* logits, int 
                     vocab, status);
 }
 cudaError_t launch_head_combine(const float2* part, int tiles, const float* z_at, const HeadRows& R, float scale, float* loss, float* total,
-                                float* block_sums, int seq, int t_pad, const HeadExact& exact, int32_t* status, cudaStream_t st) {
+                                double2* block_sums, int seq, int t_pad, const HeadExact& exact, int32_t* status, cudaStream_t st) {
   const bool few = R.rows <= COMBINE_FEW;
   const unsigned threads = !few ? 256 : (unsigned)(R.rows <= 32 ? R.rows * 32 : R.rows / 8 * 128);       // a warp has a row, or two
   return launch_pdl(exact.z ? head_combine_kernel<true> : head_combine_kernel<false>, dim3(few ? 1u : (unsigned)(R.rows / 8)), dim3(threads), 0, st,
-                    part, tiles, z_at, R, scale, loss, total, (float2*)block_sums, seq, t_pad, exact, status);
+                    part, tiles, z_at, R, scale, loss, total, block_sums, seq, t_pad, exact, status);
 }
 cudaError_t launch_head_weights(const float* dloss, const HeadRows& R, int seq, int t_pad, float inv_tau, float* raise, cudaStream_t st) {
   return launch_pdl(head_weights_kernel, dim3(1), dim3(1024), 0, st, dloss, R, seq, t_pad, inv_tau, raise);

@@ -34,7 +34,7 @@ cudaError_t launch_head_rows(int dtype, const int32_t* targets, const HeadRows& 
 cudaError_t launch_teacher_entries(const int32_t* ids, const float* logits, int top_k, float temperature, const HeadRows& R, int seq, int t_pad,
                                    int vocab, int32_t* status, cudaStream_t st);
 cudaError_t launch_head_combine(const float2* part, int tiles, const float* z_at, const HeadRows& R, float scale, float* loss, float* total,
-                                float* block_sums, int seq, int t_pad, const HeadExact& exact, int32_t* status, cudaStream_t st);
+                                double2* block_sums, int seq, int t_pad, const HeadExact& exact, int32_t* status, cudaStream_t st);
 // raise: 1 to 2, by which weights of losses are multiplied in dz and what comes of dz is divided again (see the kernel)
 cudaError_t launch_head_weights(const float* dloss, const HeadRows& R, int seq, int t_pad, float inv_tau, float* raise, cudaStream_t st);
 // dX from the areas' sums, times alpha / max(*over, 1) where `over` is not null

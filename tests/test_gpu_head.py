@@ -546,6 +546,24 @@ def test_weights_of_any_size(size, dtype):
     assert run.guards_intact() == [] and run.status() == 0
 
 
+@pytest.mark.parametrize("top_k", [0, 3])
+def test_total_is_the_losses_sum_rounded_once(top_k):
+    """Every eight rows are one block's, and here all alike, so that what a block's sum loses every block's loses: the total is the losses
+    added up in 64 bits, to half a step of fp32."""
+    for batch in (9, 11, 13, 25, 41, 63, 299):
+        c = cfg(batch, 8, 64, 500, "bf16", top_k=top_k, seed=batch)
+        inp = make_head_inputs(c)
+        for k in ("X",) + (("top_ids", "top_logits") if top_k else ("targets",)):
+            inp[k] = np.repeat(inp[k][:1], batch, axis=0)
+        run = HeadRunner(c, guard_bytes=4096)
+        run.load_inputs(inp)
+        run.forward()
+        loss, total = run.fetch("loss"), run.fetch("total")
+        assert total[1] == batch * 8
+        assert abs(total[0] - loss.sum()) <= 2.0 ** -24 * (1 + 1e-6) * loss.sum(), (batch, total[0] / loss.sum() - 1)
+        assert run.guards_intact() == []
+
+
 def test_bits_repeat_on_dirty_work_areas():
     for c in (cfg(2, 300, 256, 5003, tied=True), cfg(4, 77, 128, 1500, top_k=32, tau=2.0), cfg(2, 150, 128, 1500, "fp32")):
         inp = make_head_inputs(c, ignored=0.3)
