@@ -71,7 +71,7 @@ struct fbl_head_plan {
   int64_t w_rows;               // stored rows of W
   int top_k, tiles;             // entries a row; partials of the softmax statistics
   int logits_tile, grad_tile;   // HeadEpi.tile of the two passes
-  int piece, pieces, slices;    // columns of a piece; pieces; areas that dX's reduction is cut into
+  int piece, pieces, slices[2]; // columns of a piece; pieces; areas that dX's reduction is cut into, alone and beside dW
   int second;                   // few rows: where they lie again, for dz's second part (0: nowhere)
   int64_t x_rows;               // rows of the products
   float scale;                  // from a product to a logit times log2 e
@@ -233,21 +233,24 @@ int fbl_head_plan_create(const fbl_head_desc* desc, fbl_head_plan** out) {
   p->pieces = (p->cols + p->piece - 1) / p->piece;
   if (p->piece > p->cols) p->piece = p->cols;
 
-  // dX reduces over a piece of the vocabulary, beside dW, which reduces over the tokens: cut the former where it balances the SMs
-  {
+  // dX reduces over a piece of the vocabulary: cut it where that balances the SMs, beside dW, which reduces over the tokens, or, bf16, alone
+  // (frozen heads, us a step with the slices that go with dW, with their own, and with the best of 1 to 64: 50 tokens of 768 over 50257 columns 72,
+  // 66, 65; 10 of 2048 over 128256 268, 261, 260; 200 of 1024 over 32000 75, 77, 75; 4096 of 64 over 32000 218, 208, 208.  fp32, whose model of a
+  // launch takes areas for dearer than they are: 231 tokens of 512 over 32000 217, 252, 206; 40 of 768 over 30011 147, 165, 137)
+  for (int beside = 0; beside < 2; ++beside) {
     GemmArgs gs[2] = {dw_product(p, p->piece), dx_product(p, p->piece)};
     const int kb = (p->piece + 63) / 64;
     int want = 1;
     if (bf16) {
       const GemmShape dw = {gs[0].m, gs[0].n, (gs[0].t[0].k + 63) / 64, 0};
-      want = gemm_tc_choose_own_slices(base->sm_count, &dw, {gs[1].m, gs[1].n, kb, 1});
+      want = gemm_tc_choose_own_slices(base->sm_count, beside ? &dw : nullptr, {gs[1].m, gs[1].n, kb, 1});
     } else {
       want = gemm_tc_f32_choose_areas(base, gs, 2);
     }
     if (getenv("FBL_HEAD_SLICES") && atoi(getenv("FBL_HEAD_SLICES")) > 0) want = atoi(getenv("FBL_HEAD_SLICES"));               // likewise
     if (want > kb) want = kb;
     const int per = (kb + want - 1) / want;                                                                                   // none empty
-    p->slices = (kb + per - 1) / per;
+    p->slices[beside] = (kb + per - 1) / per;
   }
 
   const size_t n = (size_t)p->n_pad;
@@ -276,7 +279,7 @@ int fbl_head_plan_create(const fbl_head_desc* desc, fbl_head_plan** out) {
   o = FBL_ALIGN;
   p->sb_raise = take(o, 4);
   p->sb_dz = take(o, piece_bytes);
-  p->sb_acc = take(o, (size_t)p->x_rows * d.d_model * 4 * p->slices);
+  p->sb_acc = take(o, (size_t)p->x_rows * d.d_model * 4 * (p->slices[0] > p->slices[1] ? p->slices[0] : p->slices[1]));
   p->scratch_bwd_bytes = o;
   *out = p;
   return FBL_OK;
@@ -378,6 +381,7 @@ int fbl_head_bwd(const fbl_head_plan* p, const void* X, const void* W, const flo
   float* acc = (float*)(sc + p->sb_acc);
   const bool bf16 = p->d.dtype == FBL_DTYPE_BF16;
   const int D = p->d.d_model;
+  const int slices = p->slices[dW != nullptr];
   const float inv_tau = 1.f / p->d.temperature;
   // what the products of a bf16 dz are divided by: the mean's number of tokens and temperature, or what weights were multiplied by (of few
   // rows, whose dz comes in two parts, they are not)
@@ -418,11 +422,11 @@ int fbl_head_bwd(const fbl_head_plan* p, const void* X, const void* W, const flo
       g.t[0].b = weights_at(p, W, col0);
       g.t[0].b_rows = piece_rows(p, col0, cols);
       g.c = g.acc = acc;
-      g.ksplit = p->slices; g.acc_mode = col0 == 0 ? 1 : 2;
+      g.ksplit = slices; g.acc_mode = col0 == 0 ? 1 : 2;
     }
     HEAD_RUN(run_products(p, gs, count, status, st));
   }
-  if (dX) HEAD_STEP(launch_head_scatter(p->d.dtype, p->base->sm_count, acc, p->slices, R, D, bf16 ? over : nullptr, alpha, dX, st));
+  if (dX) HEAD_STEP(launch_head_scatter(p->d.dtype, p->base->sm_count, acc, slices, R, D, bf16 ? over : nullptr, alpha, dX, st));
   return FBL_OK;
 }
 

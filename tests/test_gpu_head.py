@@ -179,6 +179,39 @@ def test_frozen_sides(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("piece", [None, "1024"])
+@pytest.mark.parametrize("shape", [(1, 50, 128, 9000), (1, 7, 512, 6011), (2, 150, 128, 5003)], ids=lambda s: "x".join(map(str, s)))
+def test_gradients_together_and_alone_in_turn(monkeypatch, shape, piece, dtype):
+    """dX alone is cut into slices of its own: of one plan and one area, whatever came before it there."""
+    if piece:
+        monkeypatch.setenv("FBL_HEAD_PIECE", piece)
+    c = cfg(*shape, dtype, tied=True)
+    inp = make_head_inputs(c, ignored=0.2)
+    n = c.batch * c.seq
+    run = HeadRunner(c, guard_bytes=4096)
+    run.load_inputs(inp)
+    run.forward()
+    ref, first = orc.head_fwd_bwd(c, inp), {}
+    slack, x = dz_slack(c, inp, ref) @ np.abs(inp["W"]), inp["X"].reshape(n, -1)
+    for fill, dx, dw in ((0xFF, True, True), (0xFF, True, False), (0x7F, True, False), (0x7F, False, True), (0x7F, True, True), (0xFF, True, False)):
+        run.scratch.fill_(fill)
+        run.buf["dX"].fill_(0x11)
+        run.buf["dW"].fill_(0x11)
+        run.backward(dx=dx, dw=dw)
+        assert run.status() == 0 and run.guards_intact() == []
+        for name, on in (("dX", dx), ("dW", dw)):
+            if on:
+                got = run.fetch(name)
+                assert np.array_equal(first.setdefault((name, dx, dw), got), got)
+            else:
+                assert bool((run.buf[name] == 0x11).all())
+        if dx:
+            check_grad("dX", c, run.fetch("dX").reshape(n, -1), ref["dX"].reshape(n, -1), ref["dZ"], inp["W"], c.vocab, slack)
+        if dw:                                       # (fp32's reductions over the tokens are cut by the launch's problems, too)
+            check_grad("dW", c, run.fetch("dW").T, ref["dW"].T, x.T, ref["dZ"], n, np.abs(x.T) @ dz_slack(c, inp, ref))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("top_k", [0, 4])
 def test_no_token_has_a_loss(dtype, top_k):
     for shape in ((1, 1, 64, 300), (2, 150, 128, 1000)):
