@@ -120,6 +120,7 @@ class HeadRunner:
         if not torch.cuda.is_available():
             raise FblError(-101, "no CUDA device: the head has no CPU path")
         self.torch, self.cfg, self.dev = torch, cfg, torch.device(device)
+        self.weighted = False           # load_inputs: whether there are weights of losses
         self.plan = HeadPlan(head_desc(cfg.batch, cfg.seq, cfg.d_model, cfg.vocab, cfg.dtype, cfg.tied, cfg.top_k, cfg.temperature))
         self.tdtype = torch.float32 if cfg.dtype == "fp32" else torch.bfloat16
         al = lambda n: aligned_bytes(torch, n, self.dev, guard=guard_bytes)

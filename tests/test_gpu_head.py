@@ -628,6 +628,21 @@ def test_a_backward_may_follow_again_and_fewer_tokens_after_more():
         compare(c, inp, run)
 
 
+def test_a_runner_whose_buffers_are_filled_in_place():
+    """Without load_inputs, as behind a layer that writes X: the mean's gradient."""
+    import torch
+    c = cfg(2, 40, 128, 900)
+    inp = make_head_inputs(c, ignored=0.3)
+    a, b = HeadRunner(c, guard_bytes=4096), HeadRunner(c, guard_bytes=4096)
+    a.load_inputs(inp)
+    for n in ("X", "W"):
+        b.buf[n].copy_(a.buf[n])
+    b.vec["targets"].copy_(a.vec["targets"])
+    torch.cuda.synchronize()
+    b.step()
+    compare(c, inp, b)
+
+
 def test_padding_of_outputs_is_zero():
     import torch
     for dtype in ("bf16", "fp32"):
