@@ -456,14 +456,15 @@ int64_t fbl_norm_launch_count(const fbl_norm_plan* plan);
  * loss [batch * seq] fp32; total[0] = sum of the losses, total[1] = number of tokens with a loss (device memory, both written).
  * dloss [batch * seq] fp32, the gradient of each token's loss (of tokens without one it is not looked at), or NULL: 1 / total[1], the
  * gradient of the mean.  A factor that the weights have in common is not rounded with dz.  dX or dW may be
- * NULL: then that gradient is not formed (a frozen head; a frozen model).  The backward takes the X and W that the forward
+ * NULL: then that gradient is not formed (a frozen head; a frozen model).  The backward takes the W that the forward
  * had, and from `saved` the targets' entries, the softmax statistics and the rows of X with a loss, which the forward has brought
- * together there; `saved` serves any number of backward calls.  Outputs overlap no input and no workspace (dW is written while W
+ * together there; `saved` serves any number of backward calls.  Its X is checked as an argument and not read: the memory may serve
+ * something else by then, dX for one.  But for that outputs overlap no input and no workspace (dW is written while W
  * is still read).
  * bf16 storage: products on bf16 operands with fp32 sums; statistics, losses and gradients in fp32, dz rounded to bf16 as an
- * operand of the last two products.  Of up to 64 padded token rows dz comes in two bf16 values, its rounding and the rest, and the
- * logits at the targets enter the losses from sums in 64 bits.  The sums of dX over pieces and slices of the vocabulary are fp32, in a
- * fixed order.
+ * operand of the last two products.  Of up to 64 padded token rows dz comes in two bf16 values, its rounding and the rest, and, where
+ * rows times entries (top_k, or one label) are at most 1024, the logits at the targets enter the losses from sums in 64 bits.  The
+ * sums of dX over pieces and slices of the vocabulary are fp32, in a fixed order.
  * FBL_HEAD_PIECE, FBL_HEAD_SLICES and FBL_HEAD_TILE, read at plan creation, override the columns of a piece, the slices of dX's
  * reduction and the tile of the bf16 logits' products (for tuning and tests only). */
 typedef struct {

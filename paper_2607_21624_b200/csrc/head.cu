@@ -370,7 +370,7 @@ int fbl_head_distill_fwd(const fbl_head_plan* p, const void* X, const void* W, c
 
 int fbl_head_bwd(const fbl_head_plan* p, const void* X, const void* W, const float* dloss, const void* saved, void* dX, void* dW, void* scratch,
                  void* stream) {
-  if (!p || !X || !W || !saved || !scratch || (!dX && !dW)) return FBL_ERR_INVALID_ARG;
+  if (!p || !X || !W || !saved || !scratch || (!dX && !dW)) return FBL_ERR_INVALID_ARG;      // (X's rows with a loss are in `saved`)
   const void* ptrs[] = {X, W, saved, scratch, dX, dW};
   for (const void* q : ptrs) if (misaligned(q)) return FBL_ERR_MISALIGNED;
   cudaStream_t st = as_stream(stream);

@@ -470,6 +470,45 @@ def test_few_tokens_targets_in_64_bits(tied, top_k):
 
 
 @pytest.mark.parametrize("tied", [False, True], ids=["dv", "vd"])
+@pytest.mark.parametrize("n,top_k,exact", [(16, 64, True), (17, 64, False), (8, 128, True), (9, 128, False), (64, 16, True), (61, 17, False)])
+def test_several_targets_in_64_bits_and_where_that_ends(n, top_k, exact, tied):
+    """As above, a teacher's list of targets that hold half of the probability together, and as many rivals of 1024 exactly: up to 1024 rows
+    times entries the loss is off by what the rivals are scaled up by, (2.2e-8 + 1e-9 d) 1024 of half of it, beyond by half of the 2^-5 that
+    the targets' sums may lose as well."""
+    d, v = 4096, 2 * top_k + 3
+    c = cfg(1, n, d, v, "bf16", tied, top_k)
+    inp = make_head_inputs(c)
+    w, x = np.zeros((d, v)), np.full((1, n, d), 2.0 ** -9)
+    w[0, :2 * top_k] = x[..., 0] = 32.0
+    w[1:, top_k:2 * top_k] = 2.0 ** -8
+    inp.update(X=x, W=w.T.copy() if tied else w, top_ids=(top_k + np.array([np.random.default_rng(i).permutation(top_k) for i in range(n)])[None]).astype(np.int32))
+    ref = orc.head_fwd_bwd(c, inp)
+    run = HeadRunner(c, guard_bytes=4096)
+    run.load_inputs(inp)
+    run.forward()
+    off = np.abs(run.fetch("loss") - ref["loss"][0])
+    assert (off <= 4.4e-3 + (0.0 if exact else 2.0 ** -6)).all(), off.max()
+    assert run.guards_intact() == []
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_the_backward_does_not_read_x(dtype):
+    """dX may take X's place, and X may hold anything once the forward is done."""
+    c = cfg(2, 150, 128, 900, dtype)
+    inp = make_head_inputs(c, ignored=0.3)
+    run = HeadRunner(c)
+    run.load_inputs(inp)
+    run.step()
+    want = {k: run.fetch(k) for k in ("dX", "dW")}
+    run.buf["X"].fill_(0xFF)
+    run.buf["dX"] = run.buf["X"]
+    run.backward()
+    for k, v in want.items():
+        assert np.array_equal(v, run.fetch(k)), k
+    assert run.status() == 0
+
+
+@pytest.mark.parametrize("tied", [False, True], ids=["dv", "vd"])
 def test_fp32_operands_beyond_the_parts_range(monkeypatch, tied):
     """Hidden states of 2^100 and weights of 2^97, whose products and gradients leave the range that operands in parts have: their tiles
     are formed by multiply-adds, and the others are what they are without them."""
