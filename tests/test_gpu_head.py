@@ -745,6 +745,26 @@ def test_wide_and_long():
     run_and_compare(cfg(40, 3, 16384, 70, w_std=0.01, tied=True))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("shape,top_k", [((5, 8000, 64, 300), 0), ((11, 3333, 64, 130), 3), ((9, 8001, 64, 70), 0)],
+                         ids=lambda v: "x".join(map(str, v)) if isinstance(v, tuple) else str(v))
+def test_more_rows_than_a_block_brings_together_at_once(shape, top_k, dtype):
+    """From 32768 padded rows on a block has 64 of them and more, 32 at a time, across the ends of sequences."""
+    run_and_compare(cfg(*shape, dtype, tied=top_k > 0, top_k=top_k), ignored=0.3)
+
+
+@pytest.mark.parametrize("tied", [False, True], ids=["dv", "vd"])
+@pytest.mark.parametrize("tile", [None, "0", "1"])
+def test_pairs_in_bands_of_rows(monkeypatch, tile, tied):
+    """More than 4096 rows with a loss: a pair's tiles go in bands of eight row tiles, the last of them shorter; and fewer of them than that
+    in a launch made for more."""
+    monkeypatch.setenv("FBL_GEMM_PAIR", "1")
+    if tile:
+        monkeypatch.setenv("FBL_HEAD_TILE", tile)
+    for seq, ignored in ((4098, 0.0), (5200, 0.1), (5200, 0.5)):
+        run_and_compare(cfg(1, seq, 128, 1030, tied=tied), ignored=ignored)
+
+
 def test_weights_beyond_32_bit_offsets():
     """A head of 2.4e9 weights, labels at its end; the plain form on the GPU stands in for the oracle's time."""
     import torch
