@@ -35,10 +35,11 @@ int base_plan(int batch, int seq, int d_model, int dtype, int norm, float eps, f
   return fbl_plan_create(&ld, out);
 }
 
-// Columns of a piece.  Its logits' gradient is written once and read twice by the two products behind, so it had better stay in L2:
-// 8192 x 4096 over 32000 columns 6201 us a step with 128 MB, 6368 with 256 MB, 6280 with one piece, 6458 with 32 MB (the power cap
-// is what is felt there).  But each piece costs two launches' start and end, some 10 us: pieces of less than half a Tflop are up to
-// 256 MB (2048 x 768 over 50257 columns 348 us in one piece of 206 MB, 361 in two).
+// Columns of a piece.  Its logits' gradient is written once and read twice by the two products behind, and each piece costs two launches'
+// start and end, some 13 us.  Pieces of half a Tflop and more are of 128 MB: 8192 x 4096 over 32000 columns, in three runs that the power cap's
+// clock keeps 3 % apart, 7253 to 7263 us a step with 32 MB, 6938 to 6955 with 64 MB, 6789 to 6986 with 128 MB, 6764 to 7038 with 256 MB and 6732 to 6807
+// with one piece of 524 MB, whose memory is not worth that.  Smaller ones are up to 256 MB: 2048 x 768 over 50257 columns, a third without a
+// loss, 352 us in one piece of 206 MB, 365 in two, 377 in three, 394 in four, 438 in six.
 int64_t piece_columns(int64_t n_pad, int d_model, int e) {
   int64_t piece = ((int64_t)128 << 20) / (n_pad * e);
   const int64_t enough = (int64_t)(0.5e12 / (6.0 * (double)n_pad * d_model));
@@ -55,8 +56,8 @@ double logit_lift(int d_model) { return 2.2e-8 + 1.6e-8 * (d_model / 16); }
 }  // namespace
 
 // Products at the targets are formed again in 64 bits (exact_products) for up to so many rows and entries, which an SM's blocks hold at
-// once.  Of more tokens the errors that this takes out average out against the losses' size (2.6e-7 of their norm at 256 tokens
-// of 2048, where one token's was off by up to 1.2e-6).
+// once.  Of more tokens the errors that this takes out average out against the losses' size (2.9e-7 of their norm at 256 tokens
+// of 2048 over 32000 columns; one token's over 128256 was off by up to 3.0e-6 of itself).
 constexpr int EXACT_ROWS = 64, EXACT_ENTRIES = 1024;
 
 // Up to so many rows, half of a tile of 128, dz comes in two parts, the second below the first (head_epilogue.cuh): the rows are there

@@ -19,8 +19,8 @@ __device__ __forceinline__ void start_pass(int32_t* status) {
 }
 
 // A block forms an entry's product again, of bf16 values exactly and summed in 64 bits.  The tensor core's own sums are off by some 2^-23
-// of themselves, either way, which over many tokens averages out and of a few is what their losses are off by (one token of 2048, loss
-// 3.9: 1.9e-6, and 2e-7 with this).  It hides beside the rows' copies: a thread's loads are all on their way at once (a warp for an entry,
+// of themselves, either way, which over many tokens averages out and of a few is what their losses are off by (one token of 2048 over
+// 128256 columns, twenty draws: up to 4.2e-6, 3.0e-6 of the loss, and with this 4.7e-7, 2.5e-7 of it).  It hides beside the rows' copies: a thread's loads are all on their way at once (a warp for an entry,
 // 5 tokens of 3392 with weights by columns: 8 us more).
 template <bool TARGETS>
 __device__ __forceinline__ void exact_products(const HeadExact& E, const int32_t* __restrict__ targets, const HeadRows& R, int seq, int t_pad, int vocab,

@@ -1711,8 +1711,9 @@ int gemm_tc_logits_tile(const fbl_plan* p, int64_t m, int n, int k, int knob, in
 
 int gemm_tc_choose_own_slices(int sm_count, const GemmShape* dw, const GemmShape& dx) {
   // Few tokens: dW is bound by what it writes, dX by what it reads, and the two share the time if a third of the blocks take dX first
-  // while the others write (50 tokens of 768 over 50257 columns, 3 dX tiles: 48 units 35 us, 24 and 36 units 51 and 57, 72 to 144
-  // units 41 to 43).
+  // while the others write.  (Us a step with these slices and with the best of 1 to 48: 50 tokens of 768 over 50257 columns 90, 89; 10 of 2048
+  // over 128256 377, 360; 30 of 1024 over 32000 72, 72; 60 of 2048 over 50257 187, 183; one of 4096 over 32000 207, 199; 64 of 512 over 128256 140,
+  // 139; 20 of 4096 over 8000 88, 85; 120 of 768 over 50257 91, 90; 200 of 256 over 50257 68, 67.  One slice: 106 to 887.)
   if (dw && two_sets_pay(TILE_COST[TILE_WIDE], {dw->m, dw->n, dw->kblocks, 1})) {
     const long long tiles = (dx.m + 127) / 128 * ((dx.n + 255) / 256);
     return (int)std::max(1ll, std::min(sm_count / 3 / tiles, (long long)dx.kblocks / 8));
