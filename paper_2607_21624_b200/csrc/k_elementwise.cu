@@ -1020,6 +1020,8 @@ cudaError_t launch_norm_op_fwd(const fbl_plan* p, const void* X, const float* ga
   const int nvec = p->d.d_model / (p->d.dtype == FBL_DTYPE_FP32 ? 4 : 8);
   // (us, a block a row and a warp a row)  fp32: 592 x 2048 4.6, 5.6; 1665 x 1280 9.8, 6.0; 8192 x 2048 35.8, 26.0.  bf16, with twice the
   // instructions a byte: 16384 x 1024 17.7, 20.0; 4096 x 2048 9.7, 10.2; 1184 x 4096 7.1, 7.7; 8192 x 4096 32.1, 28.0 (LayerNorm 35.6, 33.7)
+  // Rows of more than 512 vectors find no room for two stages of twelve warps' rings and go to the block a row (one after another from L2 and
+  // memory, us): bf16 8192 x 5120 48, 8192 x 8192 61, 4096 x 16384 64, beside 26 for 8192 x 4096; fp32 8192 x 2560 43, 8192 x 4096 52, beside 23 for 8192 x 2048
   const bool fp32 = p->d.dtype == FBL_DTYPE_FP32;
   if (nvec > 512 || nvec <= (fp32 ? 96 : 384) || p->n_pad < (fp32 ? 8 : 24) * (int64_t)p->sm_count)
     return launch_norm_fwd(p, X, gamma, beta, Y, stats, nullptr, st);
