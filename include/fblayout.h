@@ -452,6 +452,8 @@ int64_t fbl_norm_launch_count(const fbl_norm_plan* plan);
  * with such ids are not there) or every logit -inf.  Their loss is 0, their rows of dX are 0 and they add nothing to dW,
  * whatever their logits: the products run over the tokens with a loss only, and what the other rows of X hold is not looked at.
  * A label or id of vocab or more, and a teacher's logit that is NaN or +inf, make the token's loss and row of dX NaN (and dW).
+ * A column whose logit is -inf has probability 0, as one that is not there (weights of it that are not finite still make dX NaN where
+ * that 0 is multiplied by them).
  *
  * loss [batch * seq] fp32; total[0] = sum of the losses, total[1] = number of tokens with a loss (device memory, both written).
  * dloss [batch * seq] fp32, the gradient of each token's loss (of tokens without one it is not looked at), or NULL: 1 / total[1], the
